@@ -246,6 +246,140 @@ cora_status cora_block_decode(cora_model *model, const int32_t *d_prompt, int32_
                               const cora_gate_cfg *gate, int32_t *d_out_tokens, int32_t *h_passes,
                               int32_t *h_total_passes, void *hip_stream);
 
+/* ---- Sampling ---------------------------------------------------------------------------
+ * A token per logits row from a given random number, device arrays of one entry per row.
+ * Over the allowed ids of a row (not mask_id, not NaN, not -inf) in the order of falling
+ * logits, equal ones by id, with w_j = exp((l_j - l_0) / temperature):
+ *   top_k > 0     keeps the first top_k;
+ *   top_p < 1     of those, the fewest whose w reach top_p of their sum (at least one);
+ *   min_p > 0     those with w >= min_p (at least one);
+ * the token is the first whose running sum of w passes u times the kept sum, 0 <= u < 1.
+ * temperature <= 0 or NaN: the first of the order (u unused).  top_k, top_p or min_p may be
+ * NULL (off for every row).  Sums are 64-bit, so the token does not depend on their order. */
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  const float *u;
+} cora_sample_rows;
+
+/* Row r of the bf16 logits [R, V] starts at d_logits + r * ld (elements, ld >= V; any
+ * alignment of 2 bytes).  mask_id = -1: no id is left out.  d_token int32 [R]; d_conf float
+ * [R] is Eq. (1)'s softmax of the token over the allowed ids at temperature 1, so that a
+ * greedy row gives cora_vocab_gate's top1 and conf.  A row without an allowed id gives token
+ * -1 and confidence 0; a NaN at an allowed id makes the row's confidence NaN.  Rows that hold
+ * +inf, NaN, or finite logits of magnitude >= 2^19 or in (0, 2^-44) that can matter take
+ * several passes.  Allocates nothing, needs no workspace.  Asynchronous. */
+cora_status cora_vocab_sample(const uint16_t *d_logits, int32_t R, int32_t V, int64_t ld,
+                              int32_t mask_id, const cora_sample_rows *rows, int32_t *d_token,
+                              float *d_conf, void *hip_stream);
+
+/* cora_vocab_gate with sampled tokens: the B * n_rows rows of the logits are drawn as by
+ * cora_vocab_sample (`rows` holds one entry per logits row, in their order) into top1 / conf,
+ * then the same decision rules run on them; persistence counts equal draws. */
+cora_status cora_vocab_gate_sampled(const uint16_t *d_logits, int32_t n_rows, int32_t row_begin,
+                                    int32_t V, int32_t mask_id, cora_state *state,
+                                    int32_t k_transfer, const cora_sched_cfg *sched,
+                                    const cora_gate_cfg *gate, const cora_sample_rows *rows,
+                                    void *hip_stream);
+
+/* ---- Paged K/V cache ----------------------------------------------------------------------
+ * Keeps the K and V of resolved positions, so that a step runs on a chunk of positions per
+ * request (its active block, a piece of its prompt, one token) instead of the whole canvas.
+ * All arrays are device memory owned by the caller.
+ *
+ * cora_cache: bf16 K and V of n_layers layers, each [n_pages, n_kv_heads, page_size * head_dim].
+ * A page of one head holds 32-key groups of 1 KB blocks in MFMA operand order; element (p, d)
+ * (position p of the page, dimension d), with k = p % 32, is at
+ *   K: (p/32) 32 hd + (k/4 % 2) 16 hd + (d/32) 512 + (d/8 % 4) 128 + (4 (k/8) + k%4) 8 + d%8
+ *   V: (p/32) 32 hd + (d/16) 512 + (k/8) 128 + (d%16) 8 + k%8.
+ * Limits: head_dim in {64, 128}; page_size 32, 64, 128 or 256; n_pages * page_size < 2^31;
+ * k and v aligned to 16 bytes. */
+typedef struct {
+  uint16_t *k, *v;
+  int32_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+} cora_cache;
+
+/* Which pages B requests hold.  table int32 [B, max_pages]: page of positions
+ * [j page_size, (j + 1) page_size); len int32 [B]: cached positions; free int32 [n_pages], a
+ * stack of the pages nobody holds, n_free int32 [1] of them.  At the start: len 0, free any
+ * permutation of 0 .. n_pages - 1, n_free n_pages (or reset, below). */
+#define CORA_CACHE_MAX_BATCH 4096
+typedef struct {
+  int32_t *table, *len, *free, *n_free;
+  int32_t B, max_pages, n_pages, page_size;
+} cora_pages;
+
+/* A chunk per request: positions [start, start + count) of each, their rows one request after
+ * another.  start, count int32 [B] are the caller's; cora_cache_plan writes cu int32 [B + 1]
+ * (request b's rows are [cu[b], cu[b+1])), status int32 [B] and, for `rows` rows, positions and
+ * slots int32 [rows] (slot = page * page_size + position in the page; both -1 in rows from
+ * cu[B] on).  `rows` is the capacity: fixed for a program, whatever the live count. */
+typedef struct {
+  const int32_t *start, *count;
+  int32_t *cu, *positions, *slots, *status;
+  int32_t rows;
+} cora_chunk;
+
+/* Block tables and slot maps from the requests' lengths, on the GPU.  First every request with
+ * count < 0 gives its pages back and its len becomes 0.  Then each request with count > 0 gets
+ * the pages that positions up to start + count need beyond those of its len, taken off the
+ * stack in the order of the requests, and len becomes max(len, start + count); a chunk inside
+ * len takes none (its positions are stored anew).  count = 0 leaves a request as it is.
+ * A request is refused, with its state left as it was, no rows and its status set, when start is
+ * negative or beyond len, or start + count beyond max_pages * page_size (CORA_ERR_INVALID_ARG);
+ * when the pages needed up to it exceed the free ones (CORA_ERR_OOM); or when the rows up to it
+ * exceed chunk->rows (CORA_ERR_UNSUPPORTED).  Status 0 otherwise.  reset != 0 forgets every
+ * request first: len 0, all pages free, page 0 handed out first.  B <= CORA_CACHE_MAX_BATCH.
+ * Allocates nothing.  Asynchronous. */
+cora_status cora_cache_plan(cora_pages *pages, cora_chunk *chunk, int32_t reset, void *hip_stream);
+
+/* Write a chunk's K and V into the pages of one layer, q and k rotated (rotate-half RoPE: pair
+ * (j, j + hd/2) of a head by the angle of the row's position).  d_x rows [q | k | v] of
+ * (n_heads + 2 n_kv_heads) head_dim elements, row stride ld: bf16 (x_f32 = 0) or fp32, rounded
+ * once.  d_rope: (cos, sin) pairs fp32 [n_pos, head_dim / 2], or NULL for rows already rotated.
+ * d_q bf16 [rows, n_heads, head_dim] receives the rotated q (NULL: not wanted).  Of the chunk,
+ * positions, slots and cu[B] are read.  Rows from cu[B] on are left alone; a row whose slot or
+ * position lies outside the cache or the table is not stored and its q is zero.  The slots of a
+ * chunk's rows must differ.  d_x, d_q, d_rope 16-byte aligned, rows too.  Asynchronous. */
+cora_status cora_cache_store(const cora_cache *cache, int32_t layer, const void *d_x, int32_t x_f32,
+                             int64_t ld, int32_t n_heads, const cora_chunk *chunk, int32_t B,
+                             const float *d_rope, int32_t n_pos, uint16_t *d_q, void *hip_stream);
+
+/* Attention of the chunk's rows over their requests' pages: query head h reads kv head
+ * h / (n_heads / n_kv_heads); keys j < len, and with causal != 0 j <= the row's position.
+ * d_q, d_out bf16 [rows, n_heads, head_dim].  A row without a key is zero; rows from cu[B] on
+ * are left alone; what the pages hold behind len is never used.  Read: chunk start, cu; pages
+ * table, len.  max_count and max_len are the most rows of a request and the longest len to
+ * expect (<= 0: rows and max_pages * page_size); they choose tiles and key ranges, and with
+ * them the order of the sums, and longer requests are still computed in full.  workspace of
+ * cora_cache_attention_workspace bytes, 16-byte aligned (NULL when that is 0): used from
+ * this call's start to its end on the stream, contents not kept; calls that may overlap and
+ * captured graphs that may run at once need one each.  Asynchronous. */
+cora_status cora_cache_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                           int32_t B, int32_t rows, int32_t max_count,
+                                           int32_t max_len, size_t *bytes);
+cora_status cora_cache_attention(const cora_cache *cache, int32_t layer, const cora_pages *pages,
+                                 const cora_chunk *chunk, const uint16_t *d_q, int32_t n_heads,
+                                 int32_t max_count, int32_t max_len, int32_t causal, float scale,
+                                 uint16_t *d_out, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream);
+
+/* The model's pass over a planned chunk against its cache: embedding of d_tokens int32
+ * [chunk->rows], every layer with its K and V stored at the chunk's slots and its queries
+ * attending to the request's pages (both directions, or causal), LM head on every row: bf16
+ * logits [rows, V].  The cache has the model's layers, kv heads and head_dim; its K holds the
+ * head's dimensions pair-interleaved (j at 2j, j + hd/2 at 2j + 1).  Rows from cu[B] on compute on
+ * whatever d_tokens holds there, their logits are unspecified.  Positions stay below max_seq
+ * (a row beyond it is not stored).  Kernel choices follow chunk->rows, B, max_count and max_len,
+ * not the live rows.  CORA_ERR_UNSUPPORTED when rows * (n_heads + 2 n_kv_heads) * head_dim
+ * exceeds the model's fp32 workspace (2^25 elements on this GPU) or rows exceed max_batch *
+ * max_seq: run a longer prompt in several chunks.  Uses the model's workspace.  Asynchronous. */
+cora_status cora_forward_cached(cora_model *model, const cora_cache *cache, const cora_pages *pages,
+                                const cora_chunk *chunk, const int32_t *d_tokens,
+                                int32_t max_count, int32_t max_len, int32_t causal,
+                                uint16_t *d_logits, void *hip_stream);
+
 /* Copy weight tensor `tensor_id` (ids as in cora_model_create) to host memory
  * in its logical row-major [out, in] layout as bf16 bits (biases too).
  * `bytes` must equal the tensor's size.  Synchronous. */

@@ -14,6 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libcora.so")
 
 c_i32, c_u64, c_f32, c_f64, c_vp, c_sz = (ctypes.c_int32, ctypes.c_uint64, ctypes.c_float,
                                           ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t)
+c_i64 = ctypes.c_int64
 
 
 class ModelCfg(ctypes.Structure):
@@ -40,6 +41,27 @@ class State(ctypes.Structure):
                 ("prompt_len", c_i32), ("gen_len", c_i32)]
 
 
+class SampleRows(ctypes.Structure):
+    _fields_ = [("temperature", c_vp), ("top_k", c_vp), ("top_p", c_vp), ("min_p", c_vp), ("u", c_vp)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", c_vp), ("v", c_vp), ("n_layers", c_i32), ("n_pages", c_i32),
+                ("n_kv_heads", c_i32), ("page_size", c_i32), ("head_dim", c_i32)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("table", c_vp), ("len", c_vp), ("free", c_vp), ("n_free", c_vp), ("B", c_i32),
+                ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32)]
+
+
+class ChunkRows(ctypes.Structure):
+    _fields_ = [("start", c_vp), ("count", c_vp), ("cu", c_vp), ("positions", c_vp),
+                ("slots", c_vp), ("status", c_vp), ("rows", c_i32)]
+
+
+_P = ctypes.POINTER
+
 EXPORTS = {
     "cora_model_create": (c_i32, [ctypes.POINTER(ModelCfg), c_u64, c_i32, c_i32, c_vp,
                                   ctypes.POINTER(c_vp)]),
@@ -54,6 +76,18 @@ EXPORTS = {
                                         c_vp]),
     "cora_block_decode": (c_i32, [c_vp, c_vp, c_i32, c_i32, c_i32, ctypes.POINTER(SchedCfg),
                                   ctypes.POINTER(GateCfg), c_vp, c_vp, c_vp, c_vp]),
+    "cora_vocab_sample": (c_i32, [c_vp, c_i32, c_i32, c_i64, c_i32, _P(SampleRows), c_vp, c_vp, c_vp]),
+    "cora_vocab_gate_sampled": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, _P(State), c_i32,
+                                        _P(SchedCfg), _P(GateCfg), _P(SampleRows), c_vp]),
+    "cora_cache_plan": (c_i32, [_P(Pages), _P(ChunkRows), c_i32, c_vp]),
+    "cora_cache_store": (c_i32, [_P(Cache), c_i32, c_vp, c_i32, c_i64, c_i32, _P(ChunkRows), c_i32,
+                                 c_vp, c_i32, c_vp, c_vp]),
+    "cora_cache_attention_workspace": (c_i32, [c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                               _P(c_sz)]),
+    "cora_cache_attention": (c_i32, [_P(Cache), c_i32, _P(Pages), _P(ChunkRows), c_vp, c_i32, c_i32,
+                                     c_i32, c_i32, c_f32, c_vp, c_vp, c_sz, c_vp]),
+    "cora_forward_cached": (c_i32, [c_vp, _P(Cache), _P(Pages), _P(ChunkRows), c_vp, c_i32, c_i32,
+                                    c_i32, c_vp, c_vp]),
     "cora_model_copy_tensor": (c_i32, [c_vp, c_i32, c_vp, c_sz]),
     "cora_model_set_timing": (c_i32, [c_vp, c_i32]),
     "cora_model_set_compaction": (c_i32, [c_vp, c_i32]),

@@ -18,7 +18,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["misc.hip", "gemm.hip", "reduce.hip", "attention.hip", "vocab_gate.hip",
-           "lm_head.hip", "runtime.hip"]
+           "lm_head.hip", "sample.hip", "cache.hip", "cache_attention.hip", "runtime.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-Wall", "-Wno-unused-function"]

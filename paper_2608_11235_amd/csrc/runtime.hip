@@ -513,6 +513,20 @@ static cora_status residual_gemm(cora_model* m, GemmArgs g, uint16_t* norm_out, 
   return CORA_OK;
 }
 
+// The rest of layer l on M rows of attention output: O projection and residual, norm, MLP, residual
+// and the next layer's norm.
+static cora_status after_attention(cora_model* m, size_t l, int M, int Mp, hipStream_t s) {
+  const auto& ly = m->layers[l];
+  const int d = m->cfg.d_model;
+  GemmArgs g{m->attn, ly.wo, W_BLOCKS, M, d, m->hq, m->h, d, nullptr, 1.0f};
+  if (cora_status st = residual_gemm(m, g, m->a, Mp, s)) return st;
+  g = GemmArgs{m->a, ly.wgu, W_BLOCKS, M, 2 * m->f_pad, d, m->u, 0, nullptr, 1.0f};
+  if (cora_status st = gemm(m, EPI_SWIGLU, g, s, m->timing)) return st;
+  g = GemmArgs{m->u, ly.wd, W_BLOCKS, M, d, m->f_pad, m->h, d, nullptr, 1.0f};
+  // the last layer's output is normalised only on the rows the LM head reads
+  return residual_gemm(m, g, l + 1 < m->layers.size() ? m->a : nullptr, Mp, s);
+}
+
 static cora_status run_layers(cora_model* m, const int32_t* tokens, int B, int L, hipStream_t s) {
   const auto& c = m->cfg;
   const int d = c.d_model, M = B * L, Ls = round_up(L, 64), Mp = plan_rows(m, L);
@@ -528,14 +542,7 @@ static cora_status run_layers(cora_model* m, const int32_t* tokens, int B, int L
     if (cora_status st = qkv_gemm(m, g, Mp, s)) return st;
     HIP_TRY(launch_attention(m->q, m->k, m->vt, m->attn, B, L, Ls, c.n_heads, c.n_kv_heads,
                              c.head_dim, m->max_batch, m->num_cus, s));
-    g = GemmArgs{m->attn, ly.wo, W_BLOCKS, M, d, m->hq, m->h, d, nullptr, 1.0f};
-    if (cora_status st = residual_gemm(m, g, m->a, Mp, s)) return st;
-    g = GemmArgs{m->a, ly.wgu, W_BLOCKS, M, 2 * m->f_pad, d, m->u, 0, nullptr, 1.0f};
-    if (cora_status st = gemm(m, EPI_SWIGLU, g, s, m->timing)) return st;
-    g = GemmArgs{m->u, ly.wd, W_BLOCKS, M, d, m->f_pad, m->h, d, nullptr, 1.0f};
-    // the last layer's output is normalised only on the rows the LM head reads
-    if (cora_status st = residual_gemm(m, g, l + 1 < n_layers ? m->a : nullptr, Mp, s))
-      return st;
+    if (cora_status st = after_attention(m, l, M, Mp, s)) return st;
   }
   return CORA_OK;
 }
@@ -916,6 +923,275 @@ extern "C" cora_status cora_block_decode(cora_model* m, const int32_t* d_prompt,
   HIP_TRY(hipStreamSynchronize(s));
   if (h_total_passes) *h_total_passes = (int32_t)total;
   return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// ---- sampling -----------------------------------------------------------------------------
+static cora_status check_sample_rows(const cora_sample_rows* r) {
+  if (!r || !r->temperature || !r->u)
+    return fail(CORA_ERR_INVALID_ARG, "null sampling rows, temperature or u");
+  return CORA_OK;
+}
+
+static SampleArgs sample_args(const uint16_t* logits, int rows, int V, int64_t ld, int mask_id,
+                              const cora_sample_rows* r, int32_t* token, float* conf) {
+  return SampleArgs{logits, rows, V, ld, mask_id, r->temperature, r->top_k, r->top_p, r->min_p, r->u,
+                    token, conf};
+}
+
+extern "C" cora_status cora_vocab_sample(const uint16_t* d_logits, int32_t R, int32_t V, int64_t ld,
+                                         int32_t mask_id, const cora_sample_rows* rows,
+                                         int32_t* d_token, float* d_conf, void* hip_stream) try {
+  if (R < 0 || V < 1 || ld < V || mask_id < -1 || mask_id >= V)
+    return fail(CORA_ERR_INVALID_ARG, "R >= 0, V >= 1, ld >= V and mask_id in [-1, V)");
+  if (V > (1 << 30)) return fail(CORA_ERR_UNSUPPORTED, "V must not exceed 2^30");
+  if (R == 0) return CORA_OK;  // no row: the arrays may be null
+  if (cora_status e = check_sample_rows(rows)) return e;
+  if (!d_logits || !d_token || !d_conf) return fail(CORA_ERR_INVALID_ARG, "null argument");
+  HIP_TRY(launch_vocab_sample(sample_args(d_logits, R, V, ld, mask_id, rows, d_token, d_conf), S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_vocab_gate_sampled(const uint16_t* d_logits, int32_t n_rows, int32_t row_begin,
+                                               int32_t V, int32_t mask_id, cora_state* st,
+                                               int32_t k_transfer, const cora_sched_cfg* sc,
+                                               const cora_gate_cfg* gt, const cora_sample_rows* rows,
+                                               void* hip_stream) try {
+  if (cora_status e = check_vocab_gate(d_logits, n_rows, row_begin, V, mask_id, st, sc, gt)) return e;
+  if (cora_status e = check_sample_rows(rows)) return e;
+  if ((int64_t)st->B * n_rows > 0x7fffffffLL) return fail(CORA_ERR_UNSUPPORTED, "B * n_rows exceeds 2^31");
+  const VocabGateArgs a = vg_args(d_logits, n_rows, row_begin, V, mask_id, st, k_transfer, sc, gt);
+  HIP_TRY(launch_vocab_sample(sample_args(d_logits, st->B * n_rows, V, V, mask_id, rows, st->top1, st->conf),
+                              S(hip_stream)));
+  HIP_TRY(launch_gate_rules(a, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// ---- paged K/V cache -------------------------------------------------------------------------
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+static int page_shift(int page_size) {  // log2, or -1
+  switch (page_size) {
+    case 32: return 5;
+    case 64: return 6;
+    case 128: return 7;
+    case 256: return 8;
+  }
+  return -1;
+}
+
+static cora_status check_cache(const cora_cache* c, int32_t layer) {
+  if (!c || !c->k || !c->v) return fail(CORA_ERR_INVALID_ARG, "null cache, k or v");
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || layer < 0 || layer >= c->n_layers)
+    return fail(CORA_ERR_INVALID_ARG, "cache dimensions must be positive, layer in [0, n_layers)");
+  if (page_shift(c->page_size) < 0)
+    return fail(CORA_ERR_UNSUPPORTED, "page_size must be 32, 64, 128 or 256");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(CORA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if ((int64_t)c->n_pages * c->page_size > 0x7fffffffLL)
+    return fail(CORA_ERR_UNSUPPORTED, "n_pages * page_size must stay below 2^31");
+  if (!aligned16(c->k) || !aligned16(c->v))
+    return fail(CORA_ERR_INVALID_ARG, "cache k and v must be aligned to 16 bytes");
+  return CORA_OK;
+}
+
+static size_t cache_layer_elems(const cora_cache* c) {
+  return (size_t)c->n_pages * c->n_kv_heads * c->page_size * c->head_dim;
+}
+
+static cora_status check_pages(const cora_pages* p) {
+  if (!p || !p->table || !p->len || !p->free || !p->n_free)
+    return fail(CORA_ERR_INVALID_ARG, "null pages array");
+  if (p->B < 1 || p->max_pages < 1 || p->n_pages < 1)
+    return fail(CORA_ERR_INVALID_ARG, "B, max_pages and n_pages must be positive");
+  if (p->B > CORA_CACHE_MAX_BATCH)
+    return fail(CORA_ERR_UNSUPPORTED, "B must not exceed CORA_CACHE_MAX_BATCH (4096)");
+  if (page_shift(p->page_size) < 0)
+    return fail(CORA_ERR_UNSUPPORTED, "page_size must be 32, 64, 128 or 256");
+  if ((int64_t)p->max_pages * p->page_size > (1 << 30) || (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
+    return fail(CORA_ERR_UNSUPPORTED, "max_pages * page_size must not exceed 2^30, n_pages * page_size 2^31 - 1");
+  return CORA_OK;
+}
+
+static cora_status check_chunk(const cora_chunk* c) {
+  if (!c || !c->start || !c->count || !c->cu || !c->positions || !c->slots || !c->status)
+    return fail(CORA_ERR_INVALID_ARG, "null chunk array");
+  if (c->rows < 0 || c->rows > (1 << 28)) return fail(CORA_ERR_INVALID_ARG, "chunk rows outside [0, 2^28]");
+  return CORA_OK;
+}
+
+static cora_status check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t rows) {
+  if (n_heads < 1 || n_kv_heads < 1) return fail(CORA_ERR_INVALID_ARG, "heads must be positive");
+  if (n_heads % n_kv_heads != 0)
+    return fail(CORA_ERR_UNSUPPORTED, "n_heads must be a multiple of n_kv_heads");
+  if (n_heads > (1 << 16) || (int64_t)rows * n_heads > (1 << 30))
+    return fail(CORA_ERR_UNSUPPORTED, "rows * n_heads must not exceed 2^30, n_heads 2^16");
+  return CORA_OK;
+}
+
+extern "C" cora_status cora_cache_plan(cora_pages* p, cora_chunk* c, int32_t reset, void* hip_stream) try {
+  if (cora_status e = check_pages(p)) return e;
+  if (cora_status e = check_chunk(c)) return e;
+  CachePlanArgs a{};
+  a.table = p->table; a.len = p->len; a.free = p->free; a.n_free = p->n_free;
+  a.start = c->start; a.count = c->count;
+  a.cu = c->cu; a.positions = c->positions; a.slots = c->slots; a.status = c->status;
+  a.B = p->B; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.shift = page_shift(p->page_size);
+  a.rows = c->rows; a.reset = reset ? 1 : 0;
+  HIP_TRY(launch_cache_plan(a, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_cache_store(const cora_cache* cache, int32_t layer, const void* d_x, int32_t x_f32,
+                                        int64_t ld, int32_t n_heads, const cora_chunk* c, int32_t B,
+                                        const float* d_rope, int32_t n_pos, uint16_t* d_q,
+                                        void* hip_stream) try {
+  if (cora_status e = check_cache(cache, layer)) return e;
+  if (cora_status e = check_chunk(c)) return e;
+  if (cora_status e = check_heads(n_heads, cache->n_kv_heads, c->rows)) return e;
+  if (!d_x || B < 1 || (d_rope && n_pos < 1)) return fail(CORA_ERR_INVALID_ARG, "null x, B < 1 or n_pos < 1");
+  const int hd = cache->head_dim;
+  if (ld < ((int64_t)n_heads + 2 * cache->n_kv_heads) * hd || ld % (x_f32 ? 4 : 8) != 0)
+    return fail(CORA_ERR_INVALID_ARG, "ld must cover a row and keep rows aligned to 16 bytes");
+  if (!aligned16(d_x) || !aligned16(d_rope) || !aligned16(d_q))
+    return fail(CORA_ERR_INVALID_ARG, "x, rope and q must be aligned to 16 bytes");
+  CacheStoreArgs a{};
+  if (x_f32) a.xf = static_cast<const float*>(d_x);
+  else a.xb = static_cast<const uint16_t*>(d_x);
+  a.ld = ld; a.splits = 1;
+  a.rows = c->rows; a.H = n_heads; a.Hkv = cache->n_kv_heads; a.shift = page_shift(cache->page_size);
+  a.n_slots = cache->n_pages * cache->page_size;
+  a.positions = c->positions; a.slots = c->slots; a.cu_end = c->cu + B;
+  a.rope = d_rope; a.n_pos = n_pos;
+  a.k = cache->k + layer * cache_layer_elems(cache);
+  a.v = cache->v + layer * cache_layer_elems(cache);
+  a.q = d_q;
+  HIP_TRY(launch_cache_store(a, hd, false, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// Compute units of the current device (256 where there is none to ask).
+static int current_cus() {
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
+    (void)hipGetLastError();
+    return 256;
+  }
+  return cus;
+}
+
+// max_count and max_len as the plan takes them
+static int expected(int32_t given, int64_t most) { return (int)(given <= 0 || given > most ? most : given); }
+
+extern "C" cora_status cora_cache_attention_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                      int32_t B, int32_t rows, int32_t max_count,
+                                                      int32_t max_len, size_t* bytes) try {
+  if (!bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
+  if (B < 1 || rows < 0 || max_len < 1) return fail(CORA_ERR_INVALID_ARG, "B >= 1, rows >= 0, max_len >= 1");
+  if (head_dim != 64 && head_dim != 128) return fail(CORA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (cora_status e = check_heads(n_heads, n_kv_heads, rows)) return e;
+  *bytes = 4 * cache_attention_plan(B, rows, n_heads, n_kv_heads, head_dim, expected(max_count, rows), max_len,
+                                    current_cus(), SIZE_MAX).ws_floats;
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_cache_attention(const cora_cache* cache, int32_t layer, const cora_pages* p,
+                                            const cora_chunk* c, const uint16_t* d_q, int32_t n_heads,
+                                            int32_t max_count, int32_t max_len, int32_t causal, float scale,
+                                            uint16_t* d_out, void* workspace, size_t workspace_bytes,
+                                            void* hip_stream) try {
+  if (cora_status e = check_cache(cache, layer)) return e;
+  if (cora_status e = check_pages(p)) return e;
+  if (cora_status e = check_chunk(c)) return e;
+  if (cora_status e = check_heads(n_heads, cache->n_kv_heads, c->rows)) return e;
+  if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
+    return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
+  if (!d_q || !d_out || !aligned16(d_q) || !aligned16(d_out))
+    return fail(CORA_ERR_INVALID_ARG, "q and out must be given, aligned to 16 bytes");
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(CORA_ERR_INVALID_ARG, "scale must be positive and finite");
+  const int hd = cache->head_dim;
+  const CacheAttnPlan pl = cache_attention_plan(
+      p->B, c->rows, n_heads, cache->n_kv_heads, hd, expected(max_count, c->rows),
+      expected(max_len, (int64_t)p->max_pages * p->page_size), current_cus(), SIZE_MAX);
+  if (pl.ws_floats && (!workspace || !aligned16(workspace) || workspace_bytes < pl.ws_floats * 4))
+    return fail(CORA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than cora_cache_attention_workspace says");
+  CacheAttnArgs a{};
+  a.q = d_q; a.out = d_out;
+  a.k = cache->k + layer * cache_layer_elems(cache);
+  a.v = cache->v + layer * cache_layer_elems(cache);
+  a.table = p->table; a.len = p->len; a.start = c->start; a.cu = c->cu;
+  a.B = p->B; a.rows = c->rows; a.H = n_heads; a.Hkv = cache->n_kv_heads; a.shift = page_shift(p->page_size);
+  a.n_pages = p->n_pages; a.max_pages = p->max_pages; a.causal = causal ? 1 : 0;
+  a.scale_log2 = LOG2E * scale;
+  HIP_TRY(launch_cache_attention(a, pl, hd, static_cast<float*>(workspace), S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// The QKV projection leaves fp32 partials in the split-K workspace; the store adds them in split
+// order, rotates, and writes q row-major and K, V into the pages; the attention then uses the same
+// workspace for its key ranges.
+extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cache, const cora_pages* p,
+                                           const cora_chunk* ch, const int32_t* d_tokens, int32_t max_count,
+                                           int32_t max_len, int32_t causal, uint16_t* d_logits,
+                                           void* hip_stream) try {
+  if (!m || !d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null argument");
+  if (cora_status e = check_cache(cache, 0)) return e;
+  if (cora_status e = check_pages(p)) return e;
+  if (cora_status e = check_chunk(ch)) return e;
+  const auto& c = m->cfg;
+  if (cache->n_layers != c.n_layers || cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim)
+    return fail(CORA_ERR_INVALID_ARG, "the cache's layers, kv heads or head_dim are not the model's");
+  if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
+    return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
+  const int M = ch->rows, d = c.d_model, hd = c.head_dim;
+  if (M == 0) return CORA_OK;
+  if ((int64_t)M > (int64_t)m->max_batch * m->max_seq || (size_t)M * m->qkv_n > m->splitk_ws_floats)
+    return fail(CORA_ERR_UNSUPPORTED, "chunk rows exceed the model's workspace: use several chunks");
+  const hipStream_t s = S(hip_stream);
+  const size_t layer_elems = cache_layer_elems(cache);
+  const CacheAttnPlan pl = cache_attention_plan(
+      p->B, M, c.n_heads, c.n_kv_heads, hd, expected(max_count, M),
+      expected(max_len, (int64_t)p->max_pages * p->page_size), m->num_cus, m->splitk_ws_floats);
+  GemmPlan gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 0, 0.0);
+  if ((size_t)gp.splits * M * m->qkv_n > m->splitk_ws_floats) gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 1, 0.0);
+  HIP_TRY(launch_embed(d_tokens, m->embed, m->h, M, d, c.vocab, m->ones, c.n_layers ? m->a : nullptr, c.rms_eps, s));
+  for (size_t l = 0; l < m->layers.size(); ++l) {
+    GemmArgs g{m->a, m->layers[l].wqkv, W_BLOCKS, M, m->qkv_n, d, m->splitk_ws, m->qkv_n, nullptr, 1.0f};
+    HIP_TRY(launch_gemm(EPI_PART_F32, g, gp, s));
+    CacheStoreArgs st{};
+    st.xf = m->splitk_ws; st.ld = m->qkv_n; st.slab = (int64_t)M * m->qkv_n; st.splits = gp.splits;
+    st.bias = m->layers[l].bqkv;
+    st.rows = M; st.H = c.n_heads; st.Hkv = c.n_kv_heads; st.shift = page_shift(cache->page_size);
+    st.n_slots = cache->n_pages * cache->page_size;
+    st.positions = ch->positions; st.slots = ch->slots; st.cu_end = ch->cu + p->B;
+    st.rope = m->rope_cs; st.n_pos = m->max_seq;
+    st.k = cache->k + l * layer_elems; st.v = cache->v + l * layer_elems; st.q = m->q;
+    HIP_TRY(launch_cache_store(st, hd, true, s));
+    CacheAttnArgs a{};
+    a.q = m->q; a.out = m->attn; a.k = st.k; a.v = st.v;
+    a.table = p->table; a.len = p->len; a.start = ch->start; a.cu = ch->cu;
+    a.B = p->B; a.rows = M; a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.shift = st.shift;
+    a.n_pages = p->n_pages; a.max_pages = p->max_pages; a.causal = causal ? 1 : 0; a.panels = 1;
+    a.scale_log2 = LOG2E / sqrtf((float)hd);
+    HIP_TRY(launch_cache_attention(a, pl, hd, m->splitk_ws, s));
+    if (cora_status e = after_attention(m, l, M, M, s)) return e;
+  }
+  const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
+  return lm_head(m, all, M, M, d_logits, s);
 } catch (...) {
   return exception_status();
 }
