@@ -15,14 +15,16 @@
 //
 // One workgroup of 1024 threads per row:
 //   1 count: one pass over the row, an LDS add per logit;
-//   2 sum:   (count, sum of w, sum of exp) of each 256-bin entry;
+//   2 sum:   count, sum of w and sum of exp of each entry of 256 bins;
 //   3 pick:  the borders n1, n2, n3 and the token's bin and rank in it, by wavefront 0: a scan of
 //            the entries, then of the 256 bins of the one that holds the border;
-//   4 find:  the rank-th id that holds the value, in a second reading of the row up to that id.
+//   4 find:  the rank-th id that holds the value, in a second reading of the row, from the end
+//            that is nearer by rank, up to that id.
 // The bins of step 1 are the bf16 numbers of magnitude 2^-44 to 2^19 of either sign and zero, 64
 // KB, so that two workgroups share a CU and one counts while the other scans.  A row with any
-// other finite number (a ban by bf16's lowest one, a maximum beyond 2^19), +inf or NaN is done by
-// the same steps over all 65536 bf16 numbers in four windows, at one reading of the row each.
+// other finite number (a maximum beyond 2^19, a logit below 2^-44), +inf or NaN is done by the same
+// steps over all 65536 bf16 numbers in four windows, at one reading of the row each; finite numbers
+// far below the maximum (a ban by bf16's lowest one), whose terms are 0 in 64 bits, do not count.
 #include <limits.h>
 
 #include <algorithm>
@@ -37,23 +39,34 @@ namespace {
 constexpr int NT = 1024, NW = NT / 64;
 constexpr int BINS = 16384, ENT = 256, NENT = BINS / ENT;  // bins in LDS, bins per entry
 constexpr uint32_t LO = 83u << 7, SPAN = 63u << 7;         // magnitudes 2^-44 <= |l| < 2^19
-constexpr int MID = (int)SPAN;                             // the bin of zero
 constexpr uint32_t FAR_BELOW = 1, OTHER = 2;               // finite numbers <= -2^19; the rest without a bin
 
-// A scheme of bins in the order of falling value.  Narrow: one window as above.
-// Wide: all bf16 numbers, window w holds bins [w BINS, (w + 1) BINS).
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2_t halves(uint32_t w) { return __builtin_bit_cast(u16x2_t, w); }
+__device__ __forceinline__ uint32_t word(u16x2_t h) { return __builtin_bit_cast(uint32_t, h); }
+
+// A scheme of bins, numbered in the order of falling value; a window of BINS of them is in LDS,
+// bin i of the window at slot(i).
+// Narrow, one window: slots 1 + magnitude - LO for positive numbers, 8192 more for negative ones,
+// 0 for zero, so that a slot is a subtraction and a bit moved.
 struct Narrow {
-  static constexpr int WINDOWS = 1, LAST = 2 * MID;
-  // bin of a number, or -1 when it has none
-  static __device__ __forceinline__ int bin(uint32_t b) {
+  static constexpr int WINDOWS = 1, LAST = BINS - 1;
+  static __device__ __forceinline__ int slot_of_bits(uint32_t b) {  // -1: none
     const uint32_t mag = b & 0x7fff, t = mag - LO;
-    const int i = (b & 0x8000) ? MID + 1 + (int)t : MID - 1 - (int)t;
-    return t < SPAN ? i : (mag == 0 ? MID : -1);
+    return t < SPAN ? (int)(((b >> 15) << 13) + 1 + t) : (mag == 0 ? 0 : -1);
   }
   static __device__ __forceinline__ uint32_t bits(int i) {
-    return i == MID ? 0u : (i < MID ? LO + (uint32_t)(MID - 1 - i) : 0x8000u | (LO + (uint32_t)(i - MID - 1)));
+    const uint32_t s = (uint32_t)(i < BINS / 2 ? BINS / 2 - 1 - i : i - BINS / 2);
+    return (i < BINS / 2 ? 0u : 0x8000u) | (s == 0 ? 0u : LO + s - 1);
+  }
+  // the counts of bins i .. i + 3, i a multiple of 4
+  static __device__ __forceinline__ u32x4_t four(const uint32_t* hist, int i) {
+    if (i >= BINS / 2) return *reinterpret_cast<const u32x4_t*>(hist + i);
+    const u32x4_t c = *reinterpret_cast<const u32x4_t*>(hist + BINS / 2 - 4 - i);
+    return u32x4_t{c[3], c[2], c[1], c[0]};
   }
 };
+// Wide, all bf16 numbers in four windows.
 struct Wide {
   static constexpr int WINDOWS = 4, LAST = 0xff7f;  // the bin of the lowest finite number
   static __device__ __forceinline__ int bin(uint32_t b) {
@@ -64,20 +77,51 @@ struct Wide {
   static __device__ __forceinline__ uint32_t bits(int i) {
     return i < 0x8000 ? 0x7fffu - (uint32_t)i : 0x8000u | (uint32_t)(i - 0x8000);
   }
+  static __device__ __forceinline__ u32x4_t four(const uint32_t* hist, int i) {
+    return *reinterpret_cast<const u32x4_t*>(hist + (i & (BINS - 1)));
+  }
 };
 
 struct Shared {
   uint32_t hist[BINS];
   uint32_t cnt[4 * NENT];
   double wt[4 * NENT], w1[4 * NENT];  // of each entry: sum of w, sum of exp
-  uint32_t first, special;            // least bin in use; FAR_BELOW, OTHER numbers without a bin
+  uint32_t tot[2][64];
+  uint32_t first[NW], special;        // least bin in use; FAR_BELOW, OTHER numbers without a bin
   int window;                         // that the histogram holds
-  uint32_t tot[2][4][NW];
-  // the pick: value, rank among its equals
-  uint32_t value, rank;
+  // the pick: value, its ids, the token's rank among them
+  uint32_t value, count, rank;
   float conf;
   int id;
 };
+
+// ---- wavefront sums by lane moves (DPP) -----------------------------------------------------
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {  // 0 where a lane has no source
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = moved<CTRL, ROWS>((uint32_t)b), hi = moved<CTRL, ROWS>((uint32_t)(b >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// inclusive sums over the lanes: inside rows of 16, then the rows before
+template <class T>
+__device__ __forceinline__ T scan(T v) {
+  v += moved<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);  // row_bcast 15, 31
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ double lane_value(double v, int l) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)lane_value((uint32_t)(b >> 32), l) << 32 | lane_value((uint32_t)b, l));
+}
 
 // Calls f(logit bits, id) for every logit of the row.
 template <class F>
@@ -86,58 +130,81 @@ __device__ __forceinline__ void each_logit(const uint16_t* x, int V, F&& f) {
   const int v0 = min((int)((0 - (uintptr_t)x) & 15) / 2, V);
   const int nch = (V - v0) >> 3, v1 = v0 + nch * 8;
   const u32x4_t* xv = reinterpret_cast<const u32x4_t*>(x + v0);
-  auto eight = [&](u32x4_t w, int c) {
+  for (int c = tid; c < nch; c += NT) {
+    const u32x4_t w = xv[c];
 #pragma unroll
     for (int j = 0; j < 8; ++j) f((j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu, v0 + c * 8 + j);
-  };
-  int c = tid;
-  for (; c + 3 * NT < nch; c += 4 * NT) {
-    u32x4_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = xv[c + i * NT];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) eight(w[i], c + i * NT);
   }
-  for (; c < nch; c += NT) eight(xv[c], c);
   if (tid < v0) f(x[tid], tid);
   if (tid < V - v1) f(x[v1 + tid], v1 + tid);
 }
 
-__device__ __forceinline__ double shfl_up_f64(double v, int o) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __shfl_up((uint32_t)b, o, 64), hi = __shfl_up((uint32_t)(b >> 32), o, 64);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
-__device__ __forceinline__ double shfl_f64(double v, int lane) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __shfl((uint32_t)b, lane, 64), hi = __shfl((uint32_t)(b >> 32), lane, 64);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
-// inclusive sums over the lanes of a wavefront
-__device__ __forceinline__ double scan_f64(double v, int lane) {
+// Step 1, Narrow.  Eight logits a load, four loads ahead; their slots by 16-bit pairs, one test for
+// all eight.  Returns FAR_BELOW / OTHER.
+__device__ __forceinline__ uint32_t count_row(Shared& sh, const uint16_t* x, int V) {
+  const int tid = threadIdx.x;
+  uint32_t special = 0;
+  auto one = [&](uint32_t b) {
+    const int s = Narrow::slot_of_bits(b);
+    if (s >= 0) atomicAdd(&sh.hist[s], 1u);
+    else if (b != 0xff80u) special |= b > 0x8000u + LO && b < 0xff80u ? FAR_BELOW : OTHER;
+  };
+  const int v0 = min((int)((0 - (uintptr_t)x) & 15) / 2, V);
+  const int nch = (V - v0) >> 3, v1 = v0 + nch * 8;
+  const u32x4_t* xv = reinterpret_cast<const u32x4_t*>(x + v0);
+  u32x4_t w[4];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = shfl_up_f64(v, o);
-    if (lane >= o) v += u;
-  }
-  return v;
-}
-
-__device__ __forceinline__ uint32_t scan_u32(uint32_t v, int lane) {
+  for (int i = 0; i < 4; ++i)
+    if (tid + i * NT < nch) w[i] = xv[tid + i * NT];
+  // the histogram is cleared while the first loads are on their way
+  u32x4_t* h = reinterpret_cast<u32x4_t*>(sh.hist);
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
+  for (int i = 0; i < BINS / 4 / NT; ++i) h[tid + i * NT] = u32x4_t{0, 0, 0, 0};
+  __syncthreads();
+  auto eight = [&](const u32x4_t& q) {
+    uint32_t at[4];
+    u16x2_t most = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u16x2_t t = halves(q[j]) - (unsigned short)LO;
+      most = __builtin_elementwise_max(most, halves(word(t) & 0x7fff7fffu));
+      // byte address of the slot before: 4 (magnitude - LO), the sign at 4 * 8192
+      at[j] = (word(t << (unsigned short)2) & 0x7ffc7ffcu) | (word(t) & 0x80008000u);
+    }
+    if (most[0] < SPAN && most[1] < SPAN) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t o = (j & 1) ? at[j >> 1] >> 16 : at[j >> 1] & 0xffffu;
+        atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sh.hist) + o) + 1, 1u);
+      }
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t p = j < 4 ? (j < 2 ? q[0] : q[1]) : (j < 6 ? q[2] : q[3]);
+        one((j & 1) ? p >> 16 : p & 0xffffu);
+      }
+    }
+  };
+  for (int c = tid; c < nch; c += 4 * NT) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ci = c + i * NT;
+      if (ci < nch) {
+        const u32x4_t q = w[i];
+        if (ci + 4 * NT < nch) w[i] = xv[ci + 4 * NT];
+        eight(q);
+      }
+    }
   }
-  return v;
+  if (tid < v0) one(x[tid]);
+  if (tid < V - v1) one(x[v1 + tid]);
+  return special;
 }
 
 // what the terms of a row are measured against
 struct Terms {
   float max;
-  double inv_t;  // 1 / T, 0 for a greedy row
+  double inv_t;  // 1 / T, -1 for a greedy row
   // l - max of a bin's number; 0 for the maximum also where that is +inf
   template <class Scheme>
   __device__ __forceinline__ double below(int bin) const {
@@ -157,8 +224,8 @@ struct Place {
   double mass, w;
 };
 
-// The histogram of one row: windows of it counted on demand, and the searches in it.  Every
-// method is called by the whole workgroup; the searches' results are wavefront 0's.
+// The histogram of one row and the searches in it.  Narrow: one wavefront may search.  Wide: the
+// whole workgroup does, since a search may have to count another window.
 template <class Scheme>
 struct Row {
   Shared& sh;
@@ -166,85 +233,68 @@ struct Row {
   int V, mask_id;
   Terms t;
   static constexpr int EPL = Scheme::WINDOWS * NENT / 64;  // entries of a lane
+  uint32_t n, ni;  // terms in this lane's entries, in those and all before
+  double s, si;    // their sums of w
 
-  __device__ void clear() {
-    u32x4_t* h = reinterpret_cast<u32x4_t*>(sh.hist);
-    for (int i = threadIdx.x; i < BINS / 4; i += NT) h[i] = u32x4_t{0, 0, 0, 0};
-  }
-
-  // counts window `win`
   __device__ void count_window(int win) {
     __syncthreads();  // everyone is done with the window before
-    clear();
+    u32x4_t* h = reinterpret_cast<u32x4_t*>(sh.hist);
+    for (int i = threadIdx.x; i < BINS / 4; i += NT) h[i] = u32x4_t{0, 0, 0, 0};
     __syncthreads();
     each_logit(x, V, [&](uint32_t b, int id) {
-      const int i = Scheme::bin(b) - win * BINS;
+      const int i = Wide::bin(b) - win * BINS;
       if (id != mask_id && (uint32_t)i < (uint32_t)BINS) atomicAdd(&sh.hist[i], 1u);
     });
     if (threadIdx.x == 0) sh.window = win;
     __syncthreads();
   }
 
-  // the entries of the window that the histogram holds
+  // Step 2 on the window that the histogram holds: the entries in use, dealt to the wavefronts.
+  // Their counts are there already.
   __device__ void sum_window(int win) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int e = wave; e < NENT; e += NW) {
-      const u32x4_t c = *reinterpret_cast<const u32x4_t*>(&sh.hist[e * ENT + lane * 4]);
-      uint32_t n = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    unsigned long long used = __ballot(sh.cnt[win * NENT + lane] != 0);
+    if (wave == 0 && !((used >> lane) & 1)) sh.wt[win * NENT + lane] = sh.w1[win * NENT + lane] = 0.0;
+    for (int k = 0; used; ++k) {
+      const int e = __ffsll(used) - 1;
+      used &= used - 1;
+      if (k % NW != wave) continue;
+      const int i0 = win * BINS + e * ENT + lane * 4;
+      const u32x4_t c = Scheme::four(sh.hist, i0);
       double st = 0.0, s1 = 0.0;
-      if (__any((c[0] | c[1] | c[2] | c[3]) != 0)) {
-#pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t cj = j == 0 ? c[0] : (j == 1 ? c[1] : (j == 2 ? c[2] : c[3]));
-          if (cj) {
-            const double d = t.template below<Scheme>(win * BINS + e * ENT + lane * 4 + j);
-            const double e1 = exp(d);
-            n += cj;
-            s1 += cj * e1;
-            st += t.inv_t == 1.0 ? cj * e1 : cj * t.weight(d);
-          }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (__any(c[j] != 0)) {
+          const double d = t.template below<Scheme>(i0 + j);
+          const double e1 = c[j] ? c[j] * exp(d) : 0.0;
+          s1 += e1;
+          if (t.inv_t == 1.0) st += e1;
+          else if (t.inv_t >= 0.0) st += c[j] ? c[j] * t.weight(d) : 0.0;
         }
-        n = scan_u32(n, lane);
-        st = scan_f64(st, lane);
-        s1 = scan_f64(s1, lane);
-      }
-      if (lane == 63) {
-        sh.cnt[win * NENT + e] = n;
+      st = lane_value(scan(st), 63);
+      s1 = lane_value(scan(s1), 63);
+      if (lane == 0) {
         sh.wt[win * NENT + e] = st;
         sh.w1[win * NENT + e] = s1;
       }
     }
   }
 
-  // The entry that holds term k of the row's order (BY_COUNT), or at which the running sum of w
-  // passes m (strict) or reaches it; and the terms and their sum before it.
-  template <bool BY_COUNT>
-  __device__ int entry_of(uint32_t k, double m, bool strict, uint32_t& before, double& mass) const {
+  // this lane's entries, after step 2; returns the row's sum of exp
+  __device__ double gather() {
     const int lane = threadIdx.x & 63;
-    uint32_t n = 0;
-    double s = 0.0;
+    double s1 = 0.0;
+    n = 0;
+    s = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       n += sh.cnt[lane * EPL + i];
       s += sh.wt[lane * EPL + i];
+      s1 += sh.w1[lane * EPL + i];
     }
-    const uint32_t ni = scan_u32(n, lane);
-    const double si = scan_f64(s, lane);
-    const int l = border(n > 0 && (BY_COUNT ? ni > k : (strict ? si > m : si >= m)), n > 0);
-    before = __shfl(ni - n, l, 64);
-    mass = l > 0 ? shfl_f64(si, l - 1) : 0.0;
-    int e = l * EPL, last = e;  // last: of the lane's entries in use
-#pragma unroll
-    for (int i = 1; i < EPL; ++i)
-      if (sh.cnt[l * EPL + i]) last = l * EPL + i;
-    for (; e < last; ++e) {
-      const uint32_t c = sh.cnt[e];
-      const double w = sh.wt[e];
-      if (c && (BY_COUNT ? before + c > k : (strict ? mass + w > m : mass + w >= m))) break;
-      before += c;
-      mass += w;
-    }
-    return e;
+    ni = scan(n);
+    si = scan(s);
+    return lane_value(scan(s1), 63);
   }
 
   // the first lane of a border, or, where rounding left the last sum short of it, the last lane in use
@@ -259,36 +309,56 @@ struct Row {
   }
 
   // this lane's four bins of entry e: their counts, w of those in use, the sums
-  __device__ __forceinline__ u32x4_t four(int e, double (&w)[4], uint32_t& n, double& s) const {
-    const int lane = threadIdx.x & 63;
-    const u32x4_t c = *reinterpret_cast<const u32x4_t*>(&sh.hist[(e % NENT) * ENT + lane * 4]);
-    n = 0;
-    s = 0.0;
-#pragma unroll 1
+  __device__ __forceinline__ u32x4_t four(int e, double (&w)[4], uint32_t& cn, double& cs) const {
+    const int i0 = e * ENT + (threadIdx.x & 63) * 4;
+    const u32x4_t c = Scheme::four(sh.hist, i0);
+    cn = 0;
+    cs = 0.0;
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t cj = j == 0 ? c[0] : (j == 1 ? c[1] : (j == 2 ? c[2] : c[3]));
-      double v = 0.0;
-      if (cj) v = t.weight(t.template below<Scheme>(e * ENT + lane * 4 + j));
-      if (j == 0) w[0] = v; else if (j == 1) w[1] = v; else if (j == 2) w[2] = v; else w[3] = v;
-      n += cj;
-      s += cj * v;
+      w[j] = 0.0;
+      if (__any(c[j] != 0)) {  // an empty bin beyond the maximum would weigh inf
+        const double v = t.weight(t.template below<Scheme>(i0 + j));
+        w[j] = c[j] ? v : 0.0;
+      }
+      cn += c[j];
+      cs += c[j] * w[j];
     }
     return c;
   }
 
-  // The bin that holds term k (BY_COUNT), or in which the running sum passes / reaches m.
+  // The bin that holds term k of the row's order (BY_COUNT), or in which the running sum of w passes
+  // m (strict) or reaches it.
   template <bool BY_COUNT>
   __device__ Place find(uint32_t k, double m, bool strict) {
-    uint32_t before = 0, n;
-    double mass = 0.0, s, w[4];
-    const int lane = threadIdx.x & 63;
-    const int e = entry_of<BY_COUNT>(k, m, strict, before, mass);
+    auto past = [&](uint32_t terms, double sum) { return BY_COUNT ? terms > k : (strict ? sum > m : sum >= m); };
+    // the entry, with what comes before it
+    int l = border(n > 0 && past(ni, si), n > 0);
+    uint32_t before = l > 0 ? lane_value(ni, l - 1) : 0;
+    double mass = l > 0 ? lane_value(si, l - 1) : 0.0;
+    int e = l * EPL;
+    if constexpr (EPL > 1) {
+      int last = e;  // of the lane's entries in use
+#pragma unroll
+      for (int i = 1; i < EPL; ++i)
+        if (sh.cnt[l * EPL + i]) last = l * EPL + i;
+      for (; e < last; ++e) {
+        const uint32_t c = sh.cnt[e];
+        const double w = sh.wt[e];
+        if (c && past(before + c, mass + w)) break;
+        before += c;
+        mass += w;
+      }
+    }
     hold(e);
-    const u32x4_t c = four(e, w, n, s);
-    const uint32_t ni = scan_u32(n, lane) + before;
-    const double si = scan_f64(s, lane) + mass;
-    const int l = border(n > 0 && (BY_COUNT ? ni > k : (strict ? si > m : si >= m)), n > 0);
-    Place p{0, ni - n, 0, si - s, 0.0};
+    // its bins
+    uint32_t cn;
+    double cs, w[4];
+    const u32x4_t c = four(e, w, cn, cs);
+    const uint32_t bi = scan(cn) + before;
+    const double mi = scan(cs) + mass;
+    l = border(cn > 0 && past(bi, mi), cn > 0);
+    Place p{0, bi - cn, 0, mi - cs, 0.0};
     bool found = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -297,42 +367,38 @@ struct Row {
         p.before += p.count;
         p.mass += p.count * p.w;
       }
-      p.bin = e * ENT + lane * 4 + j;
+      p.bin = e * ENT + (int)(threadIdx.x & 63) * 4 + j;
       p.count = c[j];
       p.w = w[j];
-      found = BY_COUNT ? p.before + c[j] > k : (strict ? p.mass + c[j] * w[j] > m : p.mass + c[j] * w[j] >= m);
+      found = past(p.before + c[j], p.mass + c[j] * w[j]);
     }
-    p.bin = __shfl(p.bin, l, 64);
-    p.before = __shfl(p.before, l, 64);
-    p.count = __shfl(p.count, l, 64);
-    p.mass = shfl_f64(p.mass, l);
-    p.w = shfl_f64(p.w, l);
-    return p;
+    return Place{(int)lane_value((uint32_t)p.bin, l), lane_value(p.before, l), lane_value(p.count, l),
+                 lane_value(p.mass, l), lane_value(p.w, l)};
   }
 
   // terms in bins up to `bin` and their sum
   __device__ uint32_t up_to(int bin, double& mass) {
     const int lane = threadIdx.x & 63, e = bin / ENT;
-    uint32_t n = 0;
-    double s = 0.0;
+    uint32_t cn = 0;
+    double cs = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
       if (lane * EPL + i < e) {
-        n += sh.cnt[lane * EPL + i];
-        s += sh.wt[lane * EPL + i];
+        cn += sh.cnt[lane * EPL + i];
+        cs += sh.wt[lane * EPL + i];
       }
     hold(e);
-    uint32_t ne;
-    double se, w[4];
-    const u32x4_t c = four(e, w, ne, se);
+    uint32_t en;
+    double es, w[4];
+    const u32x4_t c = four(e, w, en, es);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (e * ENT + lane * 4 + j <= bin) {
-        n += c[j];
-        s += c[j] * w[j];
+        cn += c[j];
+        cs += c[j] * w[j];
       }
-    mass = shfl_f64(scan_f64(s, lane), 63);
-    return __shfl(scan_u32(n, lane), 63, 64);
+    mass = lane_value(scan(cs), 63);
+    return lane_value(scan(cn), 63);
   }
 };
 
@@ -343,16 +409,21 @@ struct Settings {
   float top_p, min_p, u;
 };
 
-// Step 3, by wavefront 0 (by every wavefront where windows are counted on the way): the bin of
-// the token and its rank among that bin's ids.
+// Step 3: the bin of the token and its rank among that bin's ids.
 template <class Scheme>
-__device__ void pick(Row<Scheme>& row, int first, const Settings& g, uint32_t n, Place& p, uint32_t& rank) {
-  p = Place{first, 0, 1, 0.0, 1.0};
+__device__ void pick(Row<Scheme>& row, int first, const Settings& g, Place& p, uint32_t& rank) {
   rank = 0;
-  if (!(g.T > 0.f)) return;
-  uint32_t N = g.top_k > 0 ? min((uint32_t)g.top_k, n) : n;
-  p = row.template find<true>(N - 1, 0.0, false);
-  double mass = p.mass + (N - p.before) * p.w;  // of the first N terms
+  if (!(g.T > 0.f)) {
+    p = row.template find<true>(0, 0.0, false);
+    return;
+  }
+  uint32_t N = lane_value(row.ni, 63);
+  double mass = lane_value(row.si, 63);  // of the first N terms
+  if (g.top_k > 0 && (uint32_t)g.top_k < N) {
+    N = (uint32_t)g.top_k;
+    p = row.template find<true>(N - 1, 0.0, false);
+    mass = p.mass + (N - p.before) * p.w;
+  }
   if (g.top_p < 1.f) {
     const double m = (double)g.top_p * mass;
     p = row.template find<false>(0, m, false);
@@ -372,9 +443,9 @@ __device__ void pick(Row<Scheme>& row, int first, const Settings& g, uint32_t n,
       lo = in ? c : lo;
       hi = in ? hi : c - 1;
     }
-    double m3;
-    const uint32_t n3 = g.min_p > 1.f ? 1u : row.up_to(lo, m3);
-    if (g.min_p > 1.f) m3 = 1.0;
+    uint32_t n3 = 1;
+    double m3 = 1.0;
+    if (g.min_p <= 1.f) n3 = row.up_to(lo, m3);
     if (n3 < N) {
       N = n3;
       mass = m3;
@@ -390,98 +461,134 @@ __device__ void pick(Row<Scheme>& row, int first, const Settings& g, uint32_t n,
   }
 }
 
-// Step 4: the rank-th id that holds the value, FIND * 8 * NT ids at a time in order.
-constexpr int FIND = 4;
-__device__ void find_id(Shared& sh, const uint16_t* x, int V, int mask_id) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint32_t want = sh.value, left = sh.rank;
+// Step 4: the rank-th id that holds the value, in blocks of 4 NT chunks of eight ids, from the front
+// or from the back, the next block's loads ahead.
+__device__ __forceinline__ void find_id(Shared& sh, const uint16_t* x, int V, int mask_id) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t want = sh.value, even = want | want << 16;
+  const uint32_t care = want == 0 ? 0x7fff7fffu : 0xffffffffu;  // zeros of either sign are equal
+  const bool back = sh.rank > sh.count / 2;
+  const uint32_t left = back ? sh.count - 1 - sh.rank : sh.rank;
   const int shift = (int)((uintptr_t)x & 15) / 2;  // chunk c holds ids 8 c - shift ..
   const u32x4_t* xv = reinterpret_cast<const u32x4_t*>(x - shift);
-  const int nch = (V + shift + 7) >> 3;
+  const int nch = (V + shift + 7) >> 3, blocks = (nch + 4 * NT - 1) / (4 * NT);
+  auto whole = [&](int c) { return c * 8 >= shift && c * 8 - shift + 8 <= V; };
+  auto first_chunk = [&](int i) { return (back ? blocks - 1 - i : i) * 4 * NT + tid; };
+  u32x4_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (whole(first_chunk(0) + k * NT)) w[k] = xv[first_chunk(0) + k * NT];
   uint32_t seen = 0;
-  for (int c0 = 0, it = 0; c0 < nch; c0 += FIND * NT, it ^= 1) {
-    uint32_t hits[FIND], inc[FIND];
-    u32x4_t w[FIND];
-    bool whole[FIND];
+  for (int i = 0; i < blocks; ++i) {
+    const int c0 = first_chunk(i);
+    uint32_t hits[4];
 #pragma unroll
-    for (int k = 0; k < FIND; ++k) {
-      const int id = (c0 + k * NT + tid) * 8 - shift;
-      whole[k] = id >= 0 && id + 8 <= V;
-      if (whole[k]) w[k] = xv[c0 + k * NT + tid];
-    }
-#pragma unroll
-    for (int k = 0; k < FIND; ++k) {
-      const int id = (c0 + k * NT + tid) * 8 - shift;
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + k * NT, id = c * 8 - shift;
       hits[k] = 0;
-      if (whole[k]) {
+      if (whole(c)) {
+        u16x2_t least = {0xffff, 0xffff};
+        u16x2_t d[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t b = (j & 1) ? w[k][j >> 1] >> 16 : w[k][j >> 1] & 0xffffu;
-          hits[k] |= (uint32_t)(b == want || (want == 0 && b == 0x8000u)) << j;
+        for (int j = 0; j < 4; ++j) {
+          d[j] = halves((w[k][j] ^ even) & care);
+          least = __builtin_elementwise_min(least, d[j]);
         }
+        if (least[0] == 0 || least[1] == 0)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) hits[k] |= (uint32_t)(d[j >> 1][j & 1] == 0) << j;
       } else if (id < V) {
         for (int j = 0; j < 8; ++j)
-          if (id + j >= 0 && id + j < V) {
-            const uint32_t b = x[id + j];
-            hits[k] |= (uint32_t)(b == want || (want == 0 && b == 0x8000u)) << j;
-          }
+          if (id + j >= 0 && id + j < V) hits[k] |= (uint32_t)(((x[id + j] ^ want) & care & 0xffffu) == 0) << j;
       }
       if ((uint32_t)(mask_id - id) < 8u) hits[k] &= ~(1u << (mask_id - id));
     }
+    if (i + 1 < blocks) {
 #pragma unroll
-    for (int k = 0; k < FIND; ++k) {
+      for (int k = 0; k < 4; ++k)
+        if (whole(first_chunk(i + 1) + k * NT)) w[k] = xv[first_chunk(i + 1) + k * NT];
+    }
+    uint32_t own[4], inc[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      own[k] = __popc(hits[k]);
       inc[k] = 0;
-      if (__any(hits[k])) inc[k] = scan_u32(__popc(hits[k]), lane);
-      if (lane == 63) sh.tot[it][k][wave] = inc[k];
+      if (__any(hits[k] != 0)) inc[k] = scan(own[k]);
+      if (lane == 63) sh.tot[i & 1][k * NW + wave] = inc[k];
     }
     __syncthreads();
+    static_assert(4 * NW == 64, "a total of each wavefront and chunk to a lane");
+    const uint32_t all = scan(sh.tot[i & 1][lane]), total = lane_value(all, 63);
+    if (left < seen + total) {
+      const uint32_t at = back ? total - 1 - (left - seen) : left - seen;
 #pragma unroll
-    for (int k = 0; k < FIND; ++k) {
-      uint32_t before = seen;
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        const uint32_t c = sh.tot[it][k][i];
-        if (i < wave) before += c;
-        seen += c;
+      for (int k = 0; k < 4; ++k) {
+        const int o = k * NW + wave;
+        const uint32_t before = (o > 0 ? lane_value(all, o - 1) : 0) + inc[k] - own[k];
+        if (before <= at && at < before + own[k]) {
+          uint32_t h = hits[k];
+          for (uint32_t j = before; j < at; ++j) h &= h - 1;
+          sh.id = (c0 + k * NT) * 8 - shift + __ffs(h) - 1;
+        }
       }
-      const uint32_t own = __popc(hits[k]);
-      before += inc[k] - own;
-      if (before <= left && left < before + own) {
-        uint32_t h = hits[k];
-        for (uint32_t j = before; j < left; ++j) h &= h - 1;
-        sh.id = (c0 + k * NT + tid) * 8 - shift + __ffs(h) - 1;
-      }
+      break;
     }
-    if (seen > left) break;
+    seen += total;
   }
   __syncthreads();
 }
 
-// Steps 2 to 4 of a row that holds an allowed number; its window is counted (Narrow) or none is.
+// The counts of the window's entries and its least bin in use, dealt to the wavefronts.  A barrier
+// follows.  sh.first holds each wavefront's least bin.
 template <class Scheme>
-__device__ void draw(Shared& sh, const uint16_t* x, int V, int mask_id, int first, const Settings& g, bool nan) {
-  const int tid = threadIdx.x, lane = tid & 63;
+__device__ __forceinline__ void count_entries(Shared& sh, int win) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t least = INT_MAX;
+#pragma unroll
+  for (int k = 0; k < NENT / NW; ++k) {
+    const int e = wave * (NENT / NW) + k, i0 = win * BINS + e * ENT + lane * 4;
+    const u32x4_t c = Scheme::four(sh.hist, i0);
+    const uint32_t cn = c[0] + c[1] + c[2] + c[3];
+    const unsigned long long used = __ballot(cn != 0);
+    if (used && least == INT_MAX) {
+      const int in = c[0] ? 0 : (c[1] ? 1 : (c[2] ? 2 : 3));
+      least = lane_value((uint32_t)(i0 + in), __ffsll(used) - 1);
+    }
+    const uint32_t total = used ? lane_value(scan(cn), 63) : 0;
+    if (lane == 0) sh.cnt[win * NENT + e] = total;
+  }
+  if (lane == 0) sh.first[wave] = least;
+}
+
+__device__ __forceinline__ uint32_t least_first(const Shared& sh) {
+  uint32_t f = INT_MAX;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) f = min(f, sh.first[i]);
+  return f;
+}
+
+// Steps 2 to 4 of a row that holds an allowed number.  Narrow: its entries are counted.
+template <class Scheme>
+__device__ __forceinline__ void draw(Shared& sh, const uint16_t* x, int V, int mask_id, int first, const Settings& g, bool nan) {
   Row<Scheme> row{sh, x, V, mask_id,
-                  Terms{bf16_bits_to_f32(Scheme::bits(first)), g.T > 0.f ? 1.0 / (double)g.T : 0.0}};
+                  Terms{bf16_bits_to_f32(Scheme::bits(first)), g.T > 0.f ? 1.0 / (double)g.T : -1.0}};
   for (int w = 0; w < Scheme::WINDOWS; ++w) {
-    if (Scheme::WINDOWS > 1) row.count_window(w);
+    if (Scheme::WINDOWS > 1) {
+      row.count_window(w);
+      count_entries<Scheme>(sh, w);
+      __syncthreads();
+    }
     row.sum_window(w);
   }
   __syncthreads();
-  if (Scheme::WINDOWS > 1 || tid < 64) {
-    uint32_t n = 0, rank;
-    double s1 = 0.0;
-#pragma unroll
-    for (int i = 0; i < Row<Scheme>::EPL; ++i) {
-      n += sh.cnt[lane * Row<Scheme>::EPL + i];
-      s1 += sh.w1[lane * Row<Scheme>::EPL + i];
-    }
-    n = __shfl(scan_u32(n, lane), 63, 64);
-    s1 = shfl_f64(scan_f64(s1, lane), 63);
+  if (Scheme::WINDOWS > 1 || threadIdx.x < 64) {
+    const double s1 = row.gather();
     Place p;
-    pick<Scheme>(row, first, g, n, p, rank);
-    if (tid == 0) {
+    uint32_t rank;
+    pick<Scheme>(row, first, g, p, rank);
+    if (threadIdx.x == 0) {
       sh.value = Scheme::bits(p.bin);
+      sh.count = p.count;
       sh.rank = rank;
       sh.conf = nan ? __builtin_nanf("") : (float)(exp(row.t.template below<Scheme>(p.bin)) / s1);
       sh.id = -1;
@@ -489,6 +596,29 @@ __device__ void draw(Shared& sh, const uint16_t* x, int V, int mask_id, int firs
   }
   __syncthreads();
   find_id(sh, x, V, mask_id);
+}
+
+// A row with numbers beyond the narrow bins: maximum and NaNs of the allowed ids, then all bins.
+__device__ __forceinline__ void wide_row(Shared& sh, const uint16_t* x, int V, int mask_id, const Settings& g) {
+  __syncthreads();
+  if (threadIdx.x < NW) sh.first[threadIdx.x] = INT_MAX;
+  if (threadIdx.x == 0) { sh.special = 0; sh.window = -1; sh.id = -1; }
+  __syncthreads();
+  uint32_t first = INT_MAX;
+  bool nan = false;
+  each_logit(x, V, [&](uint32_t b, int id) {
+    if (id == mask_id) return;
+    const int i = Wide::bin(b);
+    if (i >= 0) first = min(first, (uint32_t)i);
+    else nan |= b != 0xff80u;
+  });
+  atomicMin(&sh.first[threadIdx.x >> 6], first);
+  if (nan) atomicOr(&sh.special, 1u);
+  __syncthreads();
+  first = least_first(sh);
+  nan = sh.special != 0;
+  if (first < 4u * BINS) draw<Wide>(sh, x, V, mask_id, (int)first, g, nan);
+  else if (threadIdx.x == 0) sh.conf = nan ? __builtin_nanf("") : 0.f;
 }
 
 }  // namespace
@@ -500,75 +630,26 @@ __global__ __launch_bounds__(NT, 8) void k_vocab_sample(SampleArgs a) {
   const uint16_t* x = a.logits + r * a.ld;
   const Settings g{a.temperature[r], a.top_k ? a.top_k[r] : 0, a.top_p ? a.top_p[r] : 1.f,
                    a.min_p ? a.min_p[r] : 0.f, a.u[r]};
-
-  {
-    u32x4_t* h = reinterpret_cast<u32x4_t*>(sh.hist);
-    for (int i = tid; i < BINS / 4; i += NT) h[i] = u32x4_t{0, 0, 0, 0};
-  }
-  if (tid == 0) { sh.first = INT_MAX; sh.special = 0; sh.window = 0; }
-  __syncthreads();
-  uint32_t first = INT_MAX, special = 0;
-  each_logit(x, a.V, [&](uint32_t b, int) {
-    const int i = Narrow::bin(b);
-    if (i >= 0) {
-      atomicAdd(&sh.hist[i], 1u);
-      first = min(first, (uint32_t)i);
-    } else if (b != 0xff80u) {
-      special |= b > 0x8000u + LO && b < 0xff80u ? FAR_BELOW : OTHER;
-    }
-  });
-  atomicMin(&sh.first, first);
+  if (tid == 0) { sh.special = 0; sh.window = 0; sh.id = -1; sh.conf = 0.f; }
+  uint32_t special = count_row(sh, x, a.V);  // passes a barrier before it counts
   if (special) atomicOr(&sh.special, special);
   __syncthreads();
   if (tid == 0 && a.mask_id >= 0) {  // the mask id was counted like the others: taken back
-    const int i = Narrow::bin(x[a.mask_id]);
-    if (i >= 0) sh.hist[i] -= 1;
+    const int s = Narrow::slot_of_bits(x[a.mask_id]);
+    if (s >= 0) sh.hist[s] -= 1;
   }
   __syncthreads();
-  first = sh.first;
+  count_entries<Narrow>(sh, 0);
+  __syncthreads();
+  const uint32_t first = least_first(sh);
   special = sh.special;
-  if (first < (uint32_t)BINS && sh.hist[first] == 0) {  // the mask id alone held the maximum
-    __syncthreads();
-    if (tid == 0) sh.first = INT_MAX;
-    __syncthreads();
-    uint32_t f = INT_MAX;
-    for (int i = tid; i < BINS; i += NT)
-      if (sh.hist[i]) f = min(f, (uint32_t)i);
-    atomicMin(&sh.first, f);
-    __syncthreads();
-    first = sh.first;
-  }
   // Numbers of -2^19 and below beside a maximum of at least -2^18 weigh exp(-2^18 / T), which is
   // 0 in 64 bits for T up to 350, and can then be left out.
   if (special == FAR_BELOW && g.T < 350.f && first < (uint32_t)BINS &&
       bf16_bits_to_f32(Narrow::bits((int)first)) >= -262144.f)
     special = 0;
-  if (special) {
-    // numbers beyond the narrow bins: maximum and NaNs of the allowed ids, then all bins
-    __syncthreads();
-    if (tid == 0) { sh.first = INT_MAX; sh.special = 0; sh.window = -1; }
-    __syncthreads();
-    first = INT_MAX;
-    bool nan = false;
-    each_logit(x, a.V, [&](uint32_t b, int id) {
-      if (id == a.mask_id) return;
-      const int i = Wide::bin(b);
-      if (i >= 0) first = min(first, (uint32_t)i);
-      else nan |= b != 0xff80u;
-    });
-    atomicMin(&sh.first, first);
-    if (nan) atomicOr(&sh.special, 1u);
-    __syncthreads();
-    first = sh.first;
-    nan = sh.special != 0;
-    if (first < 4u * BINS) draw<Wide>(sh, x, a.V, a.mask_id, (int)first, g, nan);
-    else if (tid == 0) { sh.id = -1; sh.conf = nan ? __builtin_nanf("") : 0.f; }
-  } else if (first < (uint32_t)BINS) {
-    draw<Narrow>(sh, x, a.V, a.mask_id, (int)first, g, false);
-  } else if (tid == 0) {
-    sh.id = -1;
-    sh.conf = 0.f;
-  }
+  if (special) wide_row(sh, x, a.V, a.mask_id, g);
+  else if (first < (uint32_t)BINS) draw<Narrow>(sh, x, a.V, a.mask_id, (int)first, g, false);
   if (tid == 0) {
     a.token[r] = sh.id;
     a.conf[r] = sh.conf;
