@@ -21,8 +21,8 @@
 //   4 find:  the rank-th id that holds the value, in a second reading of the row, from the end
 //            that is nearer by rank, up to that id.
 // The bins of step 1 are the bf16 numbers of magnitude 2^-44 to 2^19 of either sign and zero, in
-// 16-bit counts, a number and its negative to a word: 32 KB, so that four workgroups share a CU and
-// some count while others scan.  A row with any other finite number (a maximum beyond 2^19, a
+// 16-bit counts, a number and its negative to a word: 32 KB, so that three workgroups share a CU and
+// one counts while another scans.  A row with any other finite number (a maximum beyond 2^19, a
 // logit below 2^-44), +inf, NaN or more than 65535 equal logits is done by the same steps over all
 // 65536 bf16 numbers in eight windows of 32-bit counts, at one reading of the row each; finite
 // numbers far below the maximum (a ban by bf16's lowest one), whose terms are 0 in 64 bits, do not
@@ -39,6 +39,7 @@ namespace cora {
 namespace {
 
 constexpr int ENT = 256;             // bins per entry
+constexpr int BEFORE = -1, BEHIND = -2;  // instead of a chunk: a logit outside the whole ones
 constexpr uint32_t LO = 83u << 7, SPAN = 63u << 7;         // magnitudes 2^-44 <= |l| < 2^19
 constexpr uint32_t FAR_BELOW = 1, OTHER = 2;               // finite numbers <= -2^19; the rest without a bin
 
@@ -121,6 +122,7 @@ struct Shared {
   uint32_t value, count, rank;
   float conf;
   int id;
+  uint32_t first_id;
 };
 
 // ---- wavefront sums by lane moves (DPP) -----------------------------------------------------
@@ -187,20 +189,19 @@ __device__ __forceinline__ void each_logit(const uint16_t* x, int V, F&& f) {
 
 // Step 1, Narrow.  Eight logits a load, four loads ahead; their words by 16-bit pairs, one test for
 // all eight.  The mask id is counted like the others: its bin starts one below zero.  Returns
-// FAR_BELOW / OTHER; `uncounted` logits had no bin; `top` is the largest of the logits' bits as signed
-// numbers, the maximum where that is not below zero.
+// FAR_BELOW / OTHER; `uncounted` logits had no bin; `top` is the largest of this thread's logits' bits
+// as signed numbers (the maximum where that is not below zero), first seen in its chunk `top_at`.
 template <int NT, bool PAIRED, class Sh>
 __device__ __forceinline__ uint32_t count_row(Sh& sh, const uint16_t* x, int V, int mask_id, double inv_t,
-                                              uint32_t& uncounted, int& top) {
+                                              uint32_t& uncounted, int& top, int& top_at) {
   using Bins = Narrow<PAIRED>;
   const int tid = threadIdx.x;
   uint32_t special = 0;
   uncounted = 0;
-  s16x2_t high = {-32768, -32768};
   top = -32768;
+  top_at = 0;
   auto one = [&](uint32_t b) {
     const int w = Bins::place(b);
-    top = max(top, (int)(short)b);
     if (w >= 0) {
       atomicAdd(&sh.hist[w + Bins::further(b)], Bins::count(b, 1));
     } else {
@@ -234,7 +235,15 @@ __device__ __forceinline__ uint32_t count_row(Sh& sh, const uint16_t* x, int V, 
     if (tid == 0 && w >= 0) uncounted = 1;
   }
   __syncthreads();
-  auto eight = [&](const u32x4_t& q) {
+  auto eight = [&](const u32x4_t& q, int i) {
+    s16x2_t high = signed_halves(q[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) high = __builtin_elementwise_max(high, signed_halves(q[j]));
+    const int m = max((int)high[0], (int)high[1]);
+    if (m > top) {
+      top = m;
+      top_at = i;
+    }
     uint32_t t[4];  // places less one, by pairs
     u16x2_t most = {0, 0};
 #pragma unroll
@@ -247,7 +256,6 @@ __device__ __forceinline__ uint32_t count_row(Sh& sh, const uint16_t* x, int V, 
       for (int j = 0; j < 4; ++j) {
         uint32_t at = word(halves(t[j]) << (unsigned short)2);  // byte address of the word before the place's
         if (!PAIRED) at |= q[j] & 0x80008000u;
-        high = __builtin_elementwise_max(high, signed_halves(q[j]));
         auto add = [&](uint32_t o, uint32_t neg) {
           atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sh.hist) + o) + 1,
                     PAIRED ? __umul24(neg, 0xffffu) + 1u : 1u);
@@ -263,11 +271,21 @@ __device__ __forceinline__ uint32_t count_row(Sh& sh, const uint16_t* x, int V, 
       }
     }
   };
+  // the up to seven logits before the first whole chunk are a thread's each, and so are those behind
+  // the last one
+  auto edge = [&](int id, int at) {
+    one(x[id]);
+    if ((int)(short)x[id] > top) {
+      top = (int)(short)x[id];
+      top_at = at;
+    }
+  };
+  if (tid < v0) edge(tid, BEFORE);
   int i = 0;
   for (; i + 8 <= mine; i += 4) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      eight(w[k]);
+      eight(w[k], i + k);
       w[k] = xv[(i + 4 + k) * NT];
     }
   }
@@ -275,13 +293,11 @@ __device__ __forceinline__ uint32_t count_row(Sh& sh, const uint16_t* x, int V, 
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (i + k < mine) {
-        eight(w[k]);
+        eight(w[k], i + k);
         if (i + 4 + k < mine) w[k] = xv[(i + 4 + k) * NT];
       }
   }
-  if (tid < v0) one(x[tid]);
-  if (tid < V - v1) one(x[v1 + tid]);
-  top = max(top, max((int)high[0], (int)high[1]));
+  if (tid < V - v1) edge(v1 + tid, BEHIND);
   return special;
 }
 
@@ -301,7 +317,7 @@ struct Terms {
   }
   // w over T (OVER_T) or over 1 of bins i .. i + 3, i a multiple of 4; at least 0 and finite for bins
   // above the maximum too.  Narrow: neighbouring numbers of an octave are a step apart, so one
-  // exponential and three products (four exponentials each: step 2 4.8 us instead of @SUM@).
+  // exponential and three products (four exponentials each took step 2 from 3.1 to 4.5 us).
   template <class Scheme, bool OVER_T, class Sh>
   __device__ __forceinline__ void weights(const Sh& sh, int i, double (&w)[4]) const {
     if constexpr (Scheme::WINDOWS == 1) {
@@ -722,9 +738,12 @@ __device__ __forceinline__ uint32_t least_first(const Sh& sh) {
   return f;
 }
 
-// Steps 3 and 4.
+// Steps 3 and 4.  own_top: the row's maximum as its bits, where it is no less than zero and not the
+// mask id's too; top, top_at: of this thread, as count_row gives them.
+constexpr int NO_TOP = -1;
 template <class Scheme, int NT, class Sh>
-__device__ __forceinline__ void draw(Sh& sh, Row<Scheme, NT, Sh>& row, int first, const Settings& g, bool nan) {
+__device__ __forceinline__ void draw(Sh& sh, Row<Scheme, NT, Sh>& row, int first, const Settings& g, bool nan,
+                                     int own_top = NO_TOP, int top = 0, int top_at = 0) {
   if (Scheme::WINDOWS > 1 || threadIdx.x < 64) {
     const double s1 = row.gather();
     Place p;
@@ -737,9 +756,26 @@ __device__ __forceinline__ void draw(Sh& sh, Row<Scheme, NT, Sh>& row, int first
       const double d = row.t.template below<Scheme>(p.bin);
       sh.conf = nan ? __builtin_nanf("") : (float)(exp_down(sh, d) / s1);
       sh.id = -1;
+      sh.first_id = ~0u;
     }
   }
   __syncthreads();
+  if (own_top != NO_TOP && sh.rank == 0 && sh.value == (uint32_t)own_top) {
+    // the first id of the maximum, which the threads met while counting
+    if (top == own_top) {
+      const int tid = threadIdx.x, V = row.V;
+      const int v0 = min((int)((0 - (uintptr_t)row.x) & 15) / 2, V), v1 = V - ((V - v0) & 7);
+      int id = top_at == BEFORE ? tid : v1 + tid;
+      if (top_at >= 0) {
+        id = v0 + (top_at * NT + tid) * 8;
+        while ((int)(short)row.x[id] != top) ++id;
+      }
+      atomicMin(&sh.first_id, (uint32_t)id);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) sh.id = (int)sh.first_id;
+    return;
+  }
   find_id<NT>(sh, row.x, row.V, row.mask_id);
 }
 
@@ -780,7 +816,7 @@ __device__ __forceinline__ void wide_row(Shared<WORDS>& sh, const uint16_t* x, i
 }  // namespace
 
 template <int NT, bool PAIRED>
-__global__ __launch_bounds__(NT, 8) void k_vocab_sample(SampleArgs a) {
+__global__ __launch_bounds__(NT, NT == 512 ? 6 : 4) void k_vocab_sample(SampleArgs a) {
   using Bins = Narrow<PAIRED>;
   __shared__ Shared<Bins::WORDS> sh;
   const int tid = threadIdx.x;
@@ -791,19 +827,20 @@ __global__ __launch_bounds__(NT, 8) void k_vocab_sample(SampleArgs a) {
   if (tid == 0) { sh.special = sh.uncounted = 0; sh.window = 0; sh.id = -1; sh.conf = 0.f; }
   const double inv_t = g.T > 0.f ? 1.0 / (double)g.T : -1.0;  // -1: a greedy row
   uint32_t uncounted;
-  int top;
-  uint32_t special = count_row<NT, PAIRED>(sh, x, a.V, a.mask_id, inv_t, uncounted, top);  // a barrier before it counts
+  int top, top_at;
+  uint32_t special = count_row<NT, PAIRED>(sh, x, a.V, a.mask_id, inv_t, uncounted, top, top_at);  // a barrier before it counts
   if (special) atomicOr(&sh.special, special);
   if (uncounted) atomicAdd(&sh.uncounted, uncounted);
+  int most = top;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-  if ((tid & 63) == 0) sh.top[tid >> 6] = top;
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+  if ((tid & 63) == 0) sh.top[tid >> 6] = most;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) top = max(top, sh.top[i]);
+  for (int i = 0; i < NT / 64; ++i) most = max(most, sh.top[i]);
   special = sh.special;
-  const int place = top >= 0 ? Bins::place((uint32_t)top) : -1;
-  uint32_t first = place < 0 ? INT_MAX : (uint32_t)Bins::bin((uint32_t)top, place);
+  const int place = most >= 0 ? Bins::place((uint32_t)most) : -1;
+  uint32_t first = place < 0 ? INT_MAX : (uint32_t)Bins::bin((uint32_t)most, place);
   if (first == INT_MAX || Bins::four(sh.hist, first & ~3u)[first & 3] == 0) {
     // no logit above -0, or the mask id alone holds the maximum
     count_entries<Bins, NT>(sh, 0);
@@ -825,7 +862,10 @@ __global__ __launch_bounds__(NT, 8) void k_vocab_sample(SampleArgs a) {
       const uint32_t n = lane_value(scan(sh.cnt[tid & 63]), 63);
       if (n + sh.uncounted != (uint32_t)a.V) special = OTHER;
     }
-    if (!special) draw<Bins, NT>(sh, row, (int)first, g, false);
+    if (!special) {
+      const bool known = most > 0 && (a.mask_id < 0 || (int)(short)x[a.mask_id] != most);
+      draw<Bins, NT>(sh, row, (int)first, g, false, known ? most : NO_TOP, top, top_at);
+    }
   }
   if (special) wide_row<NT>(sh, x, a.V, a.mask_id, g, inv_t);
   if (tid == 0) {
@@ -836,8 +876,11 @@ __global__ __launch_bounds__(NT, 8) void k_vocab_sample(SampleArgs a) {
 
 hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  const bool small = a.rows > 512 && a.V < 65536;
-  if (small) hipLaunchKernelGGL((k_vocab_sample<512, true>), dim3(a.rows), dim3(512), 0, s, a);
+  // Up to a row per CU: 1024 threads, 32 x 126464 in 21.9 us against 25.0 with 512.  More: 512, three
+  // rows to a CU, 4096 x 126464 in 253 us against 378 with 1024 and one, 303 with 1024 in 64 registers
+  // and two, 310 with 512 in 64 registers and four (both spill); 777 x 50257 in 41.5 against 57, 54, 47.
+  const bool many = a.rows > 256;
+  if (many) hipLaunchKernelGGL((k_vocab_sample<512, true>), dim3(a.rows), dim3(512), 0, s, a);
   else hipLaunchKernelGGL((k_vocab_sample<1024, false>), dim3(a.rows), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
