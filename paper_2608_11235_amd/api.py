@@ -138,6 +138,7 @@ class Model:
         check(lib.cora_model_create(ctypes.byref(self._cfg), seed, max_batch, max_seq,
                                     stream_handle(stream), ctypes.byref(h)), "cora_model_create")
         self._h = h
+        self._device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -199,15 +200,15 @@ class Model:
                        stream=None):
         """Logits [chunk.rows, vocab] (bf16 bits) of a planned chunk against the cache, whose pages
         receive the chunk's K and V (cora_forward_cached)."""
-        check_device_tensor(tokens, "tokens", (torch.int32,), chunk.rows)
+        device = _device_of(cache, chunk)
+        if device != self._device:
+            raise ValueError(f"cache: on cuda:{device}, the model is on cuda:{self._device}")
+        rows, vocab = chunk._rows, self.spec.vocab
+        at = _checked(tokens, "tokens", _I32, rows, device)
         if out is None:
-            out = torch.empty((chunk.rows, self.spec.vocab), dtype=torch.int16, device=tokens.device)
-        check_device_tensor(out, "out", _BF16_BITS, chunk.rows * self.spec.vocab)
-        _same_device(cache.k, tokens=tokens, out=out)
-        ca, pg, ch = cache.c(), cache.pages(), chunk.c(cache)
-        check(_lib.load().cora_forward_cached(self._h, ctypes.byref(ca), ctypes.byref(pg), ctypes.byref(ch),
-                                               ptr(tokens), max_count, max_len, int(bool(causal)),
-                                               ptr(out), stream_handle(stream)), "cora_forward_cached")
+            out = _empty((rows, vocab), torch.int16, tokens.device, stream)
+        _call(device, "cora_forward_cached", self._h, cache._cache, cache._pages, chunk._chunk, at, max_count,
+              max_len, 1 if causal else 0, _checked(out, "out", _BF16_BITS, rows * vocab, device), stream=stream)
         return out
 
     def copy_tensor(self, tensor_id: int, n_elements: int) -> np.ndarray:
@@ -258,23 +259,65 @@ def vocab_gate_noalloc(logits, n_rows, row_begin, V, mask_id, state: DecodeState
           "cora_vocab_gate_noalloc")
 
 
-# ---- sampling --------------------------------------------------------------------------------
-def _same_device(first, **others):
-    """Refuse tensors of another GPU than `first`'s; None entries are skipped."""
-    for name, t in others.items():
-        if t is not None and t.device != first.device:
-            raise ValueError(f"{name}: on {t.device}, expected {first.device}")
+# ---- sampling and the paged cache ----------------------------------------------------------------
+# These calls take microseconds, so their checks test everything in one expression and look for
+# the message only when it fails.
+_F32, _I32, _U8 = (torch.float32,), (torch.int32,), (torch.uint8,)
 
 
-def _sample_rows(R, first, temperature, u, top_k, top_p, min_p):
-    f32, i32 = (torch.float32,), (torch.int32,)
-    check_device_tensor(temperature, "temperature", f32, R)
-    check_device_tensor(u, "u", f32, R)
-    for name, t, dt in (("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32)):
-        if t is not None:
-            check_device_tensor(t, name, dt, R)
-    _same_device(first, temperature=temperature, u=u, top_k=top_k, top_p=top_p, min_p=min_p)
-    return _lib.SampleRows(ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), ptr(u))
+def _checked(t, name, dtypes, numel, device):
+    """Address of a contiguous tensor of one of dtypes and at least numel elements on GPU `device`."""
+    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.get_device() == device
+            and t.is_contiguous() and t.numel() >= numel):
+        check_device_tensor(t, name, dtypes, numel)
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
+    return t.data_ptr()
+
+
+def _rows_2d(t, name, dtypes):
+    """Check a GPU matrix whose rows are contiguous; returns (device, row stride)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected two dimensions, [R, V] or [rows, width], got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected one of {dtypes}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a GPU tensor (got device {t.device})")
+    n, width = t.shape
+    if (width > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < width):
+        raise ValueError(f"{name}: strides {t.stride()}, expected rows of stride 1 that do not overlap")
+    return t.get_device(), t.stride(0) if n > 1 else width
+
+
+def _call(device, func, *args, stream=None):
+    """Call the library with `device` current, on the stream given or torch's current one there."""
+    f = getattr(_lib.load(), func)
+    if torch.cuda.current_device() == device:
+        status = f(*args, (stream or torch.cuda.current_stream(device)).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = f(*args, (stream or torch.cuda.current_stream(device)).cuda_stream)
+    if status:
+        check(status, func)
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for work on `stream`: from that stream's pool, so that nothing pending on another
+    one still uses its memory."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _sample_rows(R, device, temperature, u, top_k, top_p, min_p):
+    return _lib.SampleRows(
+        _checked(temperature, "temperature", _F32, R, device),
+        None if top_k is None else _checked(top_k, "top_k", _I32, R, device),
+        None if top_p is None else _checked(top_p, "top_p", _F32, R, device),
+        None if min_p is None else _checked(min_p, "min_p", _F32, R, device),
+        _checked(u, "u", _F32, R, device))
 
 
 def vocab_sample(logits, mask_id, temperature, u, top_k=None, top_p=None, min_p=None, token=None,
@@ -284,29 +327,16 @@ def vocab_sample(logits, mask_id, temperature, u, top_k=None, top_p=None, min_p=
     temperature, u, top_p, min_p float32 [R], top_k int32 [R]; top_k, top_p and min_p may be None.
     Rows may be strided (logits.stride(1) == 1); mask_id -1 leaves no id out.  Returns
     (token int32 [R], conf float32 [R])."""
-    if not isinstance(logits, torch.Tensor):
-        raise TypeError(f"logits: expected a torch.Tensor, got {type(logits).__name__}")
-    if logits.dim() != 2:
-        raise ValueError(f"logits: expected [R, V], got {tuple(logits.shape)}")
-    if logits.dtype not in _BF16_BITS:
-        raise TypeError(f"logits: dtype {logits.dtype}, expected one of {_BF16_BITS}")
-    if not logits.is_cuda:
-        raise ValueError(f"logits: must be a GPU tensor (got device {logits.device})")
+    device, ld = _rows_2d(logits, "logits", _BF16_BITS)
     R, V = logits.shape
-    if (V > 1 and logits.stride(1) != 1) or (R > 1 and logits.stride(0) < V):
-        raise ValueError(f"logits: strides {logits.stride()}, expected rows of stride 1 that do not overlap")
-    rows = _sample_rows(R, logits, temperature, u, top_k, top_p, min_p)
+    rows = _sample_rows(R, device, temperature, u, top_k, top_p, min_p)
     if token is None:
-        token = torch.empty(R, dtype=torch.int32, device=logits.device)
+        token = _empty(R, torch.int32, logits.device, stream)
     if conf is None:
-        conf = torch.empty(R, dtype=torch.float32, device=logits.device)
-    check_device_tensor(token, "token", (torch.int32,), R)
-    check_device_tensor(conf, "conf", (torch.float32,), R)
-    _same_device(logits, token=token, conf=conf)
-    with torch.cuda.device(logits.device):
-        check(_lib.load().cora_vocab_sample(ptr(logits), R, V, logits.stride(0) if R > 1 else V, mask_id,
-                                             ctypes.byref(rows), ptr(token), ptr(conf),
-                                             stream_handle(stream)), "cora_vocab_sample")
+        conf = _empty(R, torch.float32, logits.device, stream)
+    _call(device, "cora_vocab_sample", logits.data_ptr(), R, V, ld, mask_id, ctypes.byref(rows),
+          _checked(token, "token", _I32, R, device), _checked(conf, "conf", _F32, R, device),
+          stream=stream)
     return token, conf
 
 
@@ -314,85 +344,91 @@ def vocab_gate_sampled(logits, n_rows, row_begin, V, mask_id, state: DecodeState
                        sched: Sched, gate: Gate, temperature, u, top_k=None, top_p=None, min_p=None,
                        stream=None):
     """vocab_gate with each row's token drawn as by vocab_sample (cora_vocab_gate_sampled)."""
-    check_device_tensor(logits, "logits", _BF16_BITS, state.B * n_rows * V)
-    check_device_tensor(state.top1, "state.top1", (torch.int32,), state.B * n_rows)
-    check_device_tensor(state.conf, "state.conf", (torch.float32,), state.B * n_rows)
-    rows = _sample_rows(state.B * n_rows, logits, temperature, u, top_k, top_p, min_p)
-    _same_device(logits, **{"state.tokens": state.tokens})
+    R = state.B * n_rows
+    check_device_tensor(logits, "logits", _BF16_BITS, R * V)
+    device = logits.get_device()
+    _checked(state.top1, "state.top1", _I32, R, device)
+    _checked(state.conf, "state.conf", _F32, R, device)
+    rows = _sample_rows(R, device, temperature, u, top_k, top_p, min_p)
     st, sc, gt = state.c(), sched.c(), gate.c()
-    with torch.cuda.device(logits.device):
-        check(_lib.load().cora_vocab_gate_sampled(ptr(logits), n_rows, row_begin, V, mask_id,
-                                                   ctypes.byref(st), k_transfer, ctypes.byref(sc),
-                                                   ctypes.byref(gt), ctypes.byref(rows),
-                                                   stream_handle(stream)), "cora_vocab_gate_sampled")
+    _call(device, "cora_vocab_gate_sampled", logits.data_ptr(), n_rows, row_begin, V, mask_id,
+          ctypes.byref(st), k_transfer, ctypes.byref(sc), ctypes.byref(gt), ctypes.byref(rows),
+          stream=stream)
 
 
-# ---- paged K/V cache ---------------------------------------------------------------------------
+def _fixed(*names):
+    """Read-only attributes: the C structs hold these tensors' addresses."""
+    def add(cls):
+        for name in names:
+            setattr(cls, name, property(lambda self, key="_" + name: getattr(self, key)))
+        return cls
+    return add
+
+
+@_fixed("k", "v", "table", "len", "free", "n_free", "n_layers", "n_pages", "n_kv_heads", "head_dim",
+        "page_size", "batch", "max_pages")
 class KVCache:
     """Paged K and V of n_layers layers and the pages that up to `batch` requests hold of them
-    (cora_cache and cora_pages in include/cora.h).  Starts empty, all pages free."""
+    (cora_cache and cora_pages in include/cora.h).  Starts empty, all pages free.  Its tensors are
+    its own for good (written in place, never replaced)."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, page_size, batch, max_pages,
                  device="cuda"):
-        i32 = torch.int32
-        self.n_layers, self.n_pages, self.n_kv_heads = n_layers, n_pages, n_kv_heads
-        self.head_dim, self.page_size, self.batch, self.max_pages = head_dim, page_size, batch, max_pages
+        self._n_layers, self._n_pages, self._n_kv_heads = n_layers, n_pages, n_kv_heads
+        self._head_dim, self._page_size, self._batch, self._max_pages = head_dim, page_size, batch, max_pages
         shape = (n_layers, n_pages, n_kv_heads, page_size * head_dim)
-        self.k = torch.empty(shape, dtype=torch.bfloat16, device=device)
-        self.v = torch.empty(shape, dtype=torch.bfloat16, device=device)
-        self.table = torch.full((batch, max_pages), -1, dtype=i32, device=device)
-        self.len = torch.zeros(batch, dtype=i32, device=device)
-        self.free = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=device)
-        self.n_free = torch.full((1,), n_pages, dtype=i32, device=device)
-
-    def c(self):
-        n = self.n_layers * self.n_pages * self.n_kv_heads * self.page_size * self.head_dim
-        check_device_tensor(self.k, "cache.k", _BF16_BITS, n)
-        check_device_tensor(self.v, "cache.v", _BF16_BITS, n)
-        _same_device(self.k, **{"cache.v": self.v})
-        return _lib.Cache(ptr(self.k), ptr(self.v), self.n_layers, self.n_pages, self.n_kv_heads,
-                          self.page_size, self.head_dim)
-
-    def pages(self):
-        for name, n in (("table", self.batch * self.max_pages), ("len", self.batch),
-                        ("free", self.n_pages), ("n_free", 1)):
-            check_device_tensor(getattr(self, name), f"cache.{name}", (torch.int32,), n)
-            _same_device(self.k, **{f"cache.{name}": getattr(self, name)})
-        return _lib.Pages(ptr(self.table), ptr(self.len), ptr(self.free), ptr(self.n_free),
-                          self.batch, self.max_pages, self.n_pages, self.page_size)
+        i32 = torch.int32
+        self._k = torch.empty(shape, dtype=torch.bfloat16, device=device)
+        self._v = torch.empty(shape, dtype=torch.bfloat16, device=device)
+        self._table = torch.full((batch, max_pages), -1, dtype=i32, device=device)
+        self._len = torch.zeros(batch, dtype=i32, device=device)
+        self._free = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=device)
+        self._n_free = torch.full((1,), n_pages, dtype=i32, device=device)
+        self._device = self._k.get_device()
+        self._workspaces = {}  # bytes that cache_attention needs, by its sizes
+        self._cache = ctypes.byref(_lib.Cache(self._k.data_ptr(), self._v.data_ptr(), n_layers, n_pages,
+                                              n_kv_heads, page_size, head_dim))
+        self._pages = ctypes.byref(_lib.Pages(self._table.data_ptr(), self._len.data_ptr(),
+                                              self._free.data_ptr(), self._n_free.data_ptr(), batch,
+                                              max_pages, n_pages, page_size))
 
 
+@_fixed("start", "count", "cu", "positions", "slots", "status", "batch", "rows")
 class Chunk:
     """The rows of one pass: positions [start, start + count) of each request, up to `rows` in all
-    (cora_chunk).  The caller fills start and count; cache_plan writes the rest."""
+    (cora_chunk).  The caller writes start and count in place; cache_plan writes the rest."""
 
     def __init__(self, batch, rows, device="cuda"):
         i32 = torch.int32
-        self.batch, self.rows = batch, rows
-        self.start = torch.zeros(batch, dtype=i32, device=device)
-        self.count = torch.zeros(batch, dtype=i32, device=device)
-        self.cu = torch.zeros(batch + 1, dtype=i32, device=device)
-        self.positions = torch.full((rows,), -1, dtype=i32, device=device)
-        self.slots = torch.full((rows,), -1, dtype=i32, device=device)
-        self.status = torch.zeros(batch, dtype=i32, device=device)
+        self._batch, self._rows = batch, rows
+        self._start = torch.zeros(batch, dtype=i32, device=device)
+        self._count = torch.zeros(batch, dtype=i32, device=device)
+        self._cu = torch.zeros(batch + 1, dtype=i32, device=device)
+        self._positions = torch.full((rows,), -1, dtype=i32, device=device)
+        self._slots = torch.full((rows,), -1, dtype=i32, device=device)
+        self._status = torch.zeros(batch, dtype=i32, device=device)
+        self._device = self._start.get_device()
+        # rows = 0: torch gives no address for an empty tensor, the library asks for one
+        self._chunk = ctypes.byref(_lib.ChunkRows(
+            self._start.data_ptr(), self._count.data_ptr(), self._cu.data_ptr(),
+            self._positions.data_ptr() or self._cu.data_ptr(), self._slots.data_ptr() or self._cu.data_ptr(),
+            self._status.data_ptr(), rows))
 
-    def c(self, cache):
-        if self.batch != cache.batch:
-            raise ValueError(f"chunk: {self.batch} requests, the cache has {cache.batch}")
-        for name, n in (("start", self.batch), ("count", self.batch), ("cu", self.batch + 1),
-                        ("positions", self.rows), ("slots", self.rows), ("status", self.batch)):
-            check_device_tensor(getattr(self, name), f"chunk.{name}", (torch.int32,), n)
-            _same_device(cache.k, **{f"chunk.{name}": getattr(self, name)})
-        return _lib.ChunkRows(ptr(self.start), ptr(self.count), ptr(self.cu), ptr(self.positions),
-                              ptr(self.slots), ptr(self.status), self.rows)
+
+def _device_of(cache, chunk):
+    if cache._device < 0:
+        raise ValueError("cache: must be on a GPU")
+    if chunk._device != cache._device:
+        raise ValueError(f"chunk: not on the cache's GPU (cuda:{cache._device})")
+    if chunk._batch != cache._batch:
+        raise ValueError(f"chunk: {chunk._batch} requests, the cache has {cache._batch}")
+    return cache._device
 
 
 def cache_plan(cache: KVCache, chunk: Chunk, reset=False, stream=None):
     """Pages for the chunk and its rows' positions and slots (cora_cache_plan)."""
-    pg, ch = cache.pages(), chunk.c(cache)
-    with torch.cuda.device(cache.k.device):
-        check(_lib.load().cora_cache_plan(ctypes.byref(pg), ctypes.byref(ch), int(bool(reset)),
-                                           stream_handle(stream)), "cora_cache_plan")
+    _call(_device_of(cache, chunk), "cora_cache_plan", cache._pages, chunk._chunk, 1 if reset else 0,
+          stream=stream)
 
 
 def rope_table(n_pos, head_dim, theta, device="cuda"):
@@ -403,49 +439,42 @@ def rope_table(n_pos, head_dim, theta, device="cuda"):
     return torch.stack([torch.cos(ang), torch.sin(ang)], dim=-1).float()
 
 
+_STORED = (torch.float32,) + _BF16_BITS
+
+
 def cache_store(cache: KVCache, layer, x, n_heads, chunk: Chunk, rope=None, q=None, stream=None):
     """Rotate the q and k of x rows [q | k | v] (bf16 or float32, [rows, (n_heads + 2 n_kv_heads)
     head_dim], rows may be strided) and write K and V into the pages (cora_cache_store).  Returns q
     [rows, n_heads, head_dim] bf16; rows that the chunk does not use keep what q held."""
-    hd, Hkv = cache.head_dim, cache.n_kv_heads
-    width = (n_heads + 2 * Hkv) * hd
-    if not isinstance(x, torch.Tensor):
-        raise TypeError(f"x: expected a torch.Tensor, got {type(x).__name__}")
-    if x.dtype not in (torch.float32,) + _BF16_BITS:
-        raise TypeError(f"x: dtype {x.dtype}, expected bfloat16 or float32")
-    if not x.is_cuda:
-        raise ValueError(f"x: must be a GPU tensor (got device {x.device})")
-    if x.dim() != 2 or x.shape[0] < chunk.rows or x.shape[1] != width or x.stride(1) != 1:
-        raise ValueError(f"x: shape {tuple(x.shape)} strides {x.stride()}, the call needs "
-                         f"[{chunk.rows}, {width}] with rows of stride 1")
-    ld = x.stride(0) if x.shape[0] > 1 else width
+    device = _device_of(cache, chunk)
+    hd, rows = cache._head_dim, chunk._rows
+    width = (n_heads + 2 * cache._n_kv_heads) * hd
+    xdev, ld = _rows_2d(x, "x", _STORED)
+    if x.shape[0] < rows or x.shape[1] != width or xdev != device:
+        raise ValueError(f"x: shape {tuple(x.shape)} on {x.device}, the call needs [{rows}, {width}] on "
+                         f"cuda:{device}")
+    n_pos = 0
     if rope is not None:
-        check_device_tensor(rope, "rope", (torch.float32,))
         if rope.dim() != 3 or rope.shape[1:] != (hd // 2, 2):
             raise ValueError(f"rope: shape {tuple(rope.shape)}, expected [n_pos, {hd // 2}, 2]")
+        n_pos = rope.shape[0]
     if q is None:
-        q = torch.empty((chunk.rows, n_heads, hd), dtype=torch.bfloat16, device=x.device)
-    check_device_tensor(q, "q", _BF16_BITS, chunk.rows * n_heads * hd)
-    _same_device(cache.k, x=x, rope=rope, q=q)
-    ca, ch = cache.c(), chunk.c(cache)
-    with torch.cuda.device(x.device):
-        check(_lib.load().cora_cache_store(ctypes.byref(ca), layer, ptr(x), int(x.dtype == torch.float32),
-                                            ld, n_heads, ctypes.byref(ch), chunk.batch, ptr(rope),
-                                            0 if rope is None else rope.shape[0], ptr(q),
-                                            stream_handle(stream)), "cora_cache_store")
+        q = _empty((rows, n_heads, hd), torch.bfloat16, x.device, stream)
+    _call(device, "cora_cache_store", cache._cache, layer, x.data_ptr(), 1 if x.dtype is torch.float32 else 0,
+          ld, n_heads, chunk._chunk, chunk._batch,
+          None if rope is None else _checked(rope, "rope", _F32, 0, device), n_pos,
+          _checked(q, "q", _BF16_BITS, rows * n_heads * hd, device), stream=stream)
     return q
 
 
-def cache_attention_workspace(cache: KVCache, n_heads, chunk: Chunk, max_count, max_len):
+def cache_attention_workspace(cache: KVCache, n_heads, chunk: Chunk, max_count=0, max_len=0):
     """Bytes of workspace that cache_attention needs for these sizes."""
     n = ctypes.c_size_t(0)
-    most = cache.max_pages * cache.page_size
-    with torch.cuda.device(cache.k.device):
-        check(_lib.load().cora_cache_attention_workspace(n_heads, cache.n_kv_heads, cache.head_dim,
-                                                          cache.batch, chunk.rows, max_count,
-                                                          min(max_len, most) if max_len > 0 else most,
-                                                          ctypes.byref(n)),
-              "cora_cache_attention_workspace")
+    most = cache._max_pages * cache._page_size
+    with torch.cuda.device(cache._device):
+        check(_lib.load().cora_cache_attention_workspace(
+            n_heads, cache._n_kv_heads, cache._head_dim, cache._batch, chunk._rows, max_count,
+            min(max_len, most) if max_len > 0 else most, ctypes.byref(n)), "cora_cache_attention_workspace")
     return n.value
 
 
@@ -456,29 +485,24 @@ def cache_attention(cache: KVCache, layer, q, chunk: Chunk, max_count=0, max_len
     length to expect (0: the capacities); they choose how the work is split.  workspace: a uint8
     tensor of cache_attention_workspace bytes; by default torch's allocator provides one for the
     call.  Returns out (q's shape); rows that the chunk does not use keep what out held."""
-    check_device_tensor(q, "q", _BF16_BITS)
-    if q.dim() != 3 or q.shape[0] < chunk.rows or q.shape[2] != cache.head_dim:
-        raise ValueError(f"q: shape {tuple(q.shape)}, expected [{chunk.rows}, n_heads, {cache.head_dim}]")
+    device = _device_of(cache, chunk)
+    rows, hd = chunk._rows, cache._head_dim
+    at = _checked(q, "q", _BF16_BITS, 0, device)
+    if q.dim() != 3 or q.shape[0] < rows or q.shape[2] != hd:
+        raise ValueError(f"q: shape {tuple(q.shape)}, expected [{rows}, n_heads, {hd}]")
     n_heads = q.shape[1]
     if out is None:
-        out = torch.empty_like(q)
-    check_device_tensor(out, "out", _BF16_BITS, chunk.rows * n_heads * cache.head_dim)
-    _same_device(cache.k, q=q, out=out, workspace=workspace)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if workspace is None:
-        n = cache_attention_workspace(cache, n_heads, chunk, max_count, max_len)
+        key = (n_heads, rows, max_count, max_len)
+        n = cache._workspaces.get(key)
+        if n is None:
+            n = cache._workspaces[key] = cache_attention_workspace(cache, n_heads, chunk, max_count, max_len)
         if n:
-            workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
-    else:
-        check_device_tensor(workspace, "workspace", (torch.uint8,))
-    ca, pg, ch = cache.c(), cache.pages(), chunk.c(cache)
-    with torch.cuda.device(q.device):
-        s = stream_handle(stream)
-        check(_lib.load().cora_cache_attention(ctypes.byref(ca), layer, ctypes.byref(pg), ctypes.byref(ch),
-                                                ptr(q), n_heads, max_count, max_len, int(bool(causal)),
-                                                cache.head_dim ** -0.5 if scale is None else scale,
-                                                ptr(out), ptr(workspace),
-                                                0 if workspace is None else workspace.numel(), s),
-              "cora_cache_attention")
-        if workspace is not None and stream is not None:
-            workspace.record_stream(stream)
+            workspace = _empty(n, torch.uint8, q.device, stream)
+    _call(device, "cora_cache_attention", cache._cache, layer, cache._pages, chunk._chunk, at, n_heads,
+          max_count, max_len, 1 if causal else 0, hd ** -0.5 if scale is None else scale,
+          _checked(out, "out", _BF16_BITS, rows * n_heads * hd, device),
+          None if workspace is None else _checked(workspace, "workspace", _U8, 0, device),
+          0 if workspace is None else workspace.numel(), stream=stream)
     return out
