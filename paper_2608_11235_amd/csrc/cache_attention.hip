@@ -9,16 +9,15 @@
 // load a block, and the eight P^T slots of a lane group are eight neighbouring keys.
 //
 // The G query heads of a kv head share its K and V: the rows of a tile are (token, head) pairs,
-// token-major.  Tile t of RT rows belongs to the request b with base_b <= t < base_(b+1),
-// base_b = cu_b G / RT + b, which leaves each request at least as many tiles as it fills and needs
-// no pass over the lengths; a workgroup whose tile holds no row returns.
+// token-major.
 //
 // Two kernels.  k_cache_attend_rows (16 or 32 rows a tile): bound by the stream of K and V, each of
 // whose blocks is used by one wavefront, so they go from memory into the operand registers and the
-// four wavefronts take every fourth group of 32 keys; their states merge through LDS.
+// four wavefronts take every fourth group of 32 keys; their states merge through LDS.  The queries
+// stay in LDS, which leaves registers for three workgroups a CU at 16 rows of 128.
 // k_cache_attend_tile (64 or 128 rows): 64-key tiles through two LDS stages, loaded directly.
-// Either runs over key ranges of `chunk` keys where the rows alone would not fill the card; the
-// ranges' (max, sum, O) go to the workspace and k_cache_attend_merge folds them in order.
+// Either runs over key ranges where the rows alone would not fill the card; the ranges' (max, sum, O)
+// go to the workspace and k_cache_attend_merge folds them in order.
 #include <algorithm>
 
 #include "common.hpp"
@@ -29,6 +28,8 @@ namespace cora {
 namespace {
 
 constexpr float SLACK = 8.f;  // a reference maximum moves when a score passes it by 2^SLACK
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 __device__ __forceinline__ int clamped_cu(const CacheAttnArgs& a, int b) { return min(max(a.cu[b], 0), a.rows); }
 
@@ -48,33 +49,67 @@ __device__ __forceinline__ int owner_by_lanes(int B, int t, F first) {
   return lo + max(n, 1) - 1;
 }
 
+__device__ __forceinline__ int clamped_len(const CacheAttnArgs& a, int b) { return min(max(a.len[b], 0), a.max_pages << a.shift); }
+
+// Key ranges that a request is attended in, and the keys of each (the last has what is left): they
+// follow from its own length, never from the others in the batch.
+__device__ __forceinline__ int pieces(const CacheAttnArgs& a, int len) {
+  return min(a.splits, max(1, (int)(((int64_t)len + a.chunk - 1) / a.chunk)));
+}
+__device__ __forceinline__ int piece_keys(int len, int n) { return ((len + 31) / 32 + n - 1) / n * 32; }
+
 // What a workgroup works on: rows [row0, row0 + RT) of the (token, head) rows of request b and kv
 // head kvh, keys [k0, k1) of its `len`.
 struct Work {
   int b, kvh, split, row0, n_rows, cu, start, len, k0, k1;
 };
 
+// The first tile of a workgroup of k_cache_attend_tile; false when it has none.  Workgroups are
+// numbered with the key range slowest and from the last one on: what only long requests have starts
+// first, and the first range, which holds the short ones whole, fills the gaps at the end.  With
+// `per_request` tiles a request (every request has about as many rows) the request follows from the
+// number, the kv head the fastest.  Else (a prompt beside single tokens) tile t belongs to the request
+// b with base_b <= t < base_(b+1), base_b = cu_b G / RT + b, which leaves each request at least as many
+// tiles as it fills and needs no pass over the lengths, and an XCD takes a range of kv heads and tiles,
+// whose keys its L2 then holds.
 template <int RT>
-__device__ __forceinline__ bool work_of(const CacheAttnArgs& a, Work& w) {
-  const int li = xcd_remap(blockIdx.x, gridDim.x);
-  // later tiles see more keys under the causal mask: they start first
-  const int t = a.tiles - 1 - li % a.tiles, rest = li / a.tiles;
-  w.split = rest % a.splits;
-  w.kvh = rest / a.splits;
-  const int G = a.G;
-  w.b = __builtin_amdgcn_readfirstlane(
-      owner_by_lanes(a.B, t, [&](int b) { return (int)((int64_t)clamped_cu(a, b) * G / RT) + b; }));
-  w.cu = clamped_cu(a, w.b);
-  const int n = clamped_cu(a, w.b + 1) - w.cu;
-  w.n_rows = n * G;
-  w.row0 = (t - (int)((int64_t)w.cu * G / RT) - w.b) * RT;
+__device__ __forceinline__ bool first_tile(const CacheAttnArgs& a, Work& w) {
+  int li = blockIdx.x;
+  if (a.per_request > 0) {
+    w.kvh = li % a.Hkv;
+    li /= a.Hkv;
+    w.row0 = li % a.per_request * RT;
+    li /= a.per_request;
+    w.b = li % a.B;
+    w.split = a.splits - 1 - li / a.B;
+  } else {
+    const int n = a.tiles * a.Hkv;
+    w.split = a.splits - 1 - li / n;
+    li = xcd_remap(li % n, n);
+    const int t = a.tiles - 1 - li % a.tiles;  // later tiles see more keys under the causal mask: they start first
+    w.kvh = li / a.tiles;
+    w.b = uniform(owner_by_lanes(a.B, t, [&](int b) { return (int)((int64_t)clamped_cu(a, b) * a.G / RT) + b; }));
+    w.row0 = (t - (int)((int64_t)uniform(clamped_cu(a, w.b)) * a.G / RT) - w.b) * RT;
+  }
+  w.cu = uniform(clamped_cu(a, w.b));
+  w.n_rows = (uniform(clamped_cu(a, w.b + 1)) - w.cu) * a.G;
   if (w.row0 >= w.n_rows) return false;
-  w.start = a.start[w.b];
-  w.len = min(max(a.len[w.b], 0), a.max_pages << a.shift);
-  w.k0 = w.split * a.chunk;
-  if (w.split > 0 && w.k0 >= w.len) return false;
-  w.k1 = w.split == a.splits - 1 ? w.len : min(w.len, w.k0 + a.chunk);
+  w.start = uniform(a.start[w.b]);
+  w.len = uniform(clamped_len(a, w.b));
+  const int n = pieces(a, w.len);
+  if (w.split >= n) return false;
+  const int each = (piece_keys(w.len, n) + 63) / 64 * 64;
+  w.k0 = w.split * each;
+  w.k1 = min(w.len, w.k0 + each);
   return true;
+}
+
+// The next one: a request with more rows than its tiles were made for takes several turns.
+template <int RT>
+__device__ __forceinline__ bool next_tile(const CacheAttnArgs& a, Work& w) {
+  if (a.per_request == 0) return false;
+  w.row0 += a.per_request * RT;
+  return w.row0 < w.n_rows;
 }
 
 // keys that row `row` sees; rows behind the last one, whose results nobody reads, as many as it
@@ -84,20 +119,23 @@ __device__ __forceinline__ int limit_of(const CacheAttnArgs& a, const Work& w, i
   return min((int64_t)w.len, max((int64_t)w.start + row / a.G + 1, (int64_t)0));
 }
 
-// The page of 32-key group `grp` of the request, 64 table entries held in the lanes.
-struct PageList {
-  const int32_t* table;
-  int shift5, n_pages, max_pages, base, mine;  // shift5: log2 of 32-key groups a page
-  __device__ __forceinline__ void load(int page) {
-    base = page;
-    const int p = page + (int)(threadIdx.x & 63);
-    mine = p < max_pages ? table[p] : 0;
-  }
-  __device__ __forceinline__ int page(int grp) {
-    const int p = grp >> shift5;
-    if (p - base >= 64) load(p);
-    const int e = __builtin_amdgcn_readlane(mine, p - base);
-    return (unsigned)e < (unsigned)n_pages ? e : 0;  // a bad entry reads page 0, never past the pool
+// Where the 32-key groups of one request and kv head lie.  The block table is read by scalar loads:
+// they are counted apart from the vector loads in flight, so that a page can be looked up between
+// those of K and V without waiting for them, and an entry is read a group before its use.
+template <int HD>
+struct Groups {
+  const __attribute__((address_space(4))) int32_t* table;
+  int shift5, mask5, n_pages;  // log2 of 32-key groups a page, that less one
+  int64_t page_bytes, head_bytes;
+  __device__ __forceinline__ Groups(const CacheAttnArgs& a, const Work& w)
+      : table((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (int64_t)w.b * a.max_pages)),
+        shift5(a.shift - 5), mask5((1 << (a.shift - 5)) - 1), n_pages(a.n_pages),
+        page_bytes((int64_t)a.Hkv * HD * 2 << a.shift), head_bytes((int64_t)w.kvh * HD * 2 << a.shift) {}
+  __device__ __forceinline__ int entry(int grp) const { return table[uniform(grp >> shift5)]; }
+  // byte offset in the pool of a group of that entry; a bad entry reads page 0, never past the pool
+  __device__ __forceinline__ int64_t offset(int entry, int grp) const {
+    const int page = (unsigned)entry < (unsigned)n_pages ? entry : 0;
+    return page * page_bytes + head_bytes + (int64_t)(grp & mask5) * (32 * HD * 2);
   }
 };
 
@@ -200,24 +238,63 @@ __device__ __forceinline__ int64_t out_index(const CacheAttnArgs& a, int token, 
   return ((int64_t)(c >> 5) * a.rows + token) * 32 + (c & 31);
 }
 
+// The result of RB x 16 rows from row `first` of the workgroup on, or their part of it.
+template <int HD, int RB>
+__device__ __forceinline__ void store_rows(const CacheAttnArgs& a, const Work& w, int first, const float (&m_ref)[RB],
+                                           const float (&l)[RB], const f32x4_t (&o)[RB][HD / 16]) {
+  constexpr int ND = HD / 16;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float s = l[rb];
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    const int row = w.row0 + first + rb * 16 + r16;
+    if (row >= w.n_rows) continue;
+    const int token = w.cu + row / a.G, head = w.kvh * a.G + row % a.G;
+    if (pieces(a, w.len) == 1) {  // the whole of the request's keys
+      const float inv = s == 0.f ? 0.f : 1.0f / s;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+        *reinterpret_cast<u32x2_t*>(a.out + out_index(a, token, head, d * 16 + g * 4, HD)) =
+            u32x2_t{pack_bf16x2(o[rb][d][0] * inv, o[rb][d][1] * inv), pack_bf16x2(o[rb][d][2] * inv, o[rb][d][3] * inv)};
+    } else {
+      const int64_t p = ((int64_t)token * a.H + head) * a.splits + w.split;
+      if (g == 0) {
+        a.part_ml[2 * p] = m_ref[rb];
+        a.part_ml[2 * p + 1] = s;
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4_t*>(a.part_o + p * HD + d * 16 + g * 4) = o[rb][d];
+    }
+  }
+}
+
 }  // namespace
 
 template <int HD, int RB>
-__global__ __launch_bounds__(256) void k_cache_attend_rows(CacheAttnArgs a) {
-  constexpr int RT = RB * 16, NK = HD / 32, ND = HD / 16, LDO = HD + 4;
-  __shared__ float so[4][RT][LDO];
-  __shared__ float sm[4][RT], sl[4][RT];
-  Work w;
-  if (!work_of<RT>(a, w)) return;
+struct RowsShared {
+  u32x4_t q[RB * (HD / 32)][64];
+  f32x4_t o[2][RB * (HD / 16)][64];
+  float m[2][RB][64], l[2][RB][64];
+};
+
+template <int HD, int RB>
+__device__ __forceinline__ void attend_rows(const CacheAttnArgs& a, const Work& w, RowsShared<HD, RB>& sh) {
+  constexpr int NK = HD / 32, ND = HD / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, r16 = lane & 15;
 
-  bf16x8_t qf[RB][NK];
   int lim[RB], most = 0;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int row = w.row0 + rb * 16 + r16;
-    load_q<HD>(a, w, row, qf[rb]);
+    if (wave == rb) {
+      bf16x8_t qf[NK];
+      load_q<HD>(a, w, row, qf);
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) sh.q[rb * NK + kk][lane] = __builtin_bit_cast(u32x4_t, qf[kk]);
+    }
     lim[rb] = limit_of(a, w, row);
     most = max(most, lim[rb]);
   }
@@ -235,26 +312,37 @@ __global__ __launch_bounds__(256) void k_cache_attend_rows(CacheAttnArgs a) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[rb][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int64_t head_elems = (int64_t)HD << a.shift;
-  PageList pl{a.table + (int64_t)w.b * a.max_pages, a.shift - 5, a.n_pages, a.max_pages, 0, 0};
-  const int gmask = (1 << (a.shift - 5)) - 1;
-  auto at = [&](int grp) -> int64_t {  // element offset of a 32-key group in the pool
-    return ((int64_t)pl.page(grp) * a.Hkv + w.kvh) * head_elems + (int64_t)(grp & gmask) * (32 * HD) + lane * 8;
-  };
+  __syncthreads();
+  const Groups<HD> groups(a, w);
+  // K and V are read once, past the caches' regular places (non-temporal): 46 us against 55 for the
+  // ragged tokens, 22.6 against 25.2 for the blocks.
+  // Per group: V's loads go out first, S^T waits for K's, which were sent a group ago; then the next
+  // K's loads take the registers that S^T has read, and O^T waits for V's.
   u32x4_t kf[2 * NK], vf[ND];
-  int grp = g0 + wave;
-  if (grp < g1) {
-    pl.load(grp >> pl.shift5);
-    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(a.k + at(grp));
+  auto load_k = [&](int64_t at) {
+    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(a.k) + at) + lane;
 #pragma unroll
-    for (int i = 0; i < 2 * NK; ++i) kf[i] = p[i * 64];
+    for (int i = 0; i < 2 * NK; ++i) kf[i] = __builtin_nontemporal_load(p + i * 64);
+  };
+  int grp = g0 + wave;
+  int64_t here = 0;
+  int entry = 0;
+  if (grp < g1) {
+    here = groups.offset(groups.entry(grp), grp);
+    load_k(here);
+    entry = groups.entry(min(grp + 4, g1 - 1));
   }
   for (; grp < g1; grp += 4) {
+    // the last time once more the same: no branch, so that V's waits count on K's loads
+    const int next = grp + 4 < g1 ? grp + 4 : grp;
+    const int64_t ahead = groups.offset(entry, next);
+    entry = groups.entry(min(grp + 8, g1 - 1));
     {
-      const u32x4_t* p = reinterpret_cast<const u32x4_t*>(a.v + at(grp));
+      const u32x4_t* p = reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(a.v) + here) + lane;
 #pragma unroll
-      for (int i = 0; i < ND; ++i) vf[i] = p[i * 64];
+      for (int i = 0; i < ND; ++i) vf[i] = __builtin_nontemporal_load(p + i * 64);
     }
+    __builtin_amdgcn_sched_barrier(0);
     f32x4_t st[RB][2];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
@@ -263,13 +351,11 @@ __global__ __launch_bounds__(256) void k_cache_attend_rows(CacheAttnArgs a) {
         st[rb][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk)
-          st[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[kb * NK + kk]), qf[rb][kk], st[rb][kb], 0, 0, 0);
+          st[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[kb * NK + kk]), as_bf16x8(sh.q[rb * NK + kk][lane]), st[rb][kb], 0, 0, 0);
       }
-    if (grp + 4 < g1) {
-      const u32x4_t* p = reinterpret_cast<const u32x4_t*>(a.k + at(grp + 4));
-#pragma unroll
-      for (int i = 0; i < 2 * NK; ++i) kf[i] = p[i * 64];
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(ahead);
+    __builtin_amdgcn_sched_barrier(0);
     const int key = grp * 32 + 8 * g;  // of the lane's first term
     bool cut = false;                  // some row's last key lies in the group
 #pragma unroll
@@ -304,66 +390,106 @@ __global__ __launch_bounds__(256) void k_cache_attend_rows(CacheAttnArgs a) {
     if (__any(bad)) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
-        add_non_finite<ND>(a.v + at(grp) - lane * 8, st[rb][0], st[rb][1], min(lim[rb], w.k1) - grp * 32, o[rb]);
+        add_non_finite<ND>(reinterpret_cast<const uint16_t*>(reinterpret_cast<const char*>(a.v) + here), st[rb][0], st[rb][1], min(lim[rb], w.k1) - grp * 32, o[rb]);
     }
+    here = ahead;
   }
 
+  // wavefronts 2 and 3 hand their states to 0 and 1, and 1 to 0, lane by lane
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    float s = l[rb];
-    s += __shfl_xor(s, 16, 64);
-    s += __shfl_xor(s, 32, 64);
-    const int row = rb * 16 + r16;
-    if (g == 0) {
-      sm[wave][row] = m_ref[rb];
-      sl[wave][row] = s;
-    }
+  for (int from = 2; from > 0; from >>= 1) {
+    if (wave >= from && wave < 2 * from) {
 #pragma unroll
-    for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4_t*>(&so[wave][row][d * 16 + g * 4]) = o[rb][d];
-  }
-  __syncthreads();
-  // thread: 4 dimensions of a row at a time
-  constexpr int TPR = HD / 4;
-  for (int i = threadIdx.x; i < RT * TPR; i += 256) {
-    const int r = i / TPR, d = (i % TPR) * 4, row = w.row0 + r;
-    if (row >= w.n_rows) continue;
-    const float m = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
-    float sum = 0.f;
-    f32x4_t x{0.f, 0.f, 0.f, 0.f};
+      for (int rb = 0; rb < RB; ++rb) {
+        sh.m[wave - from][rb][lane] = m_ref[rb];
+        sh.l[wave - from][rb][lane] = l[rb];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const float c = sm[v][r] == -INFINITY ? 0.f : fast_exp2(sm[v][r] - m);
-      // a wavefront that saw no key, unlike one that saw a NaN, adds nothing
-      if (sm[v][r] == -INFINITY && sl[v][r] == 0.f) continue;
-      sum += sl[v][r] * (sm[v][r] == -INFINITY ? 1.f : c);
-      x += *reinterpret_cast<const f32x4_t*>(&so[v][r][d]) * (sm[v][r] == -INFINITY ? 1.f : c);
-    }
-    const int token = w.cu + row / a.G, head = w.kvh * a.G + row % a.G;
-    if (a.splits == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      *reinterpret_cast<u32x2_t*>(a.out + out_index(a, token, head, d, HD)) =
-          u32x2_t{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
-    } else {
-      const int64_t p = ((int64_t)token * a.H + head) * a.splits + w.split;
-      if (d == 0) {
-        a.part_ml[2 * p] = m;
-        a.part_ml[2 * p + 1] = sum;
+        for (int d = 0; d < ND; ++d) sh.o[wave - from][rb * ND + d][lane] = o[rb][d];
       }
-      *reinterpret_cast<f32x4_t*>(a.part_o + p * HD + d) = x;
     }
+    __syncthreads();
+    if (wave < from) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float m1 = sh.m[wave][rb][lane], m = fmaxf(m_ref[rb], m1);
+        // a state that saw no key is (-inf, 0, 0), or holds a NaN that has to stay one
+        const float c0 = m_ref[rb] == m ? 1.f : fast_exp2(m_ref[rb] - m), c1 = m1 == m ? 1.f : fast_exp2(m1 - m);
+        m_ref[rb] = m;
+        l[rb] = l[rb] * c0 + sh.l[wave][rb][lane] * c1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[rb][d] = o[rb][d] * c0 + sh.o[wave][rb * ND + d][lane] * c1;
+      }
+    }
+    __syncthreads();  // the LDS is free again
+  }
+  if (wave == 0) store_rows<HD, RB>(a, w, 0, m_ref, l, o);
+}
+
+// The work is a list of (request, key range, tile, kv head).  Every workgroup adds up the requests'
+// counts and takes every gridDim'th entry: the list holds no empty ones, where a grid over the ranges
+// of the longest request took 27 us to start for 64 ragged tokens, half of it for nothing.
+template <int HD, int RB>
+__global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
+  constexpr int RT = RB * 16;
+  extern __shared__ uint32_t first[];  // [B + 1]: pieces of the requests before
+  __shared__ uint32_t part[4];
+  __shared__ RowsShared<HD, RB> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  uint32_t carry = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 256) {
+    const int b = b0 + tid;
+    uint32_t n = 0;
+    if (b < a.B) {
+      const int rows = (clamped_cu(a, b + 1) - clamped_cu(a, b)) * a.G, len = clamped_len(a, b);
+      if (rows > 0)
+        n = (uint32_t)((rows + RT - 1) / RT) * (uint32_t)a.Hkv * (uint32_t)pieces(a, len);
+    }
+    uint32_t s = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t u = __shfl_up(s, o, 64);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) part[wave] = s;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < wave) s += part[i];
+    }
+    if (b < a.B) first[b] = carry + s - n;
+    carry += part[0] + part[1] + part[2] + part[3];
+    __syncthreads();
+  }
+  const uint32_t total = uniform(carry);
+  for (uint32_t i = blockIdx.x; i < total; i += gridDim.x) {
+    Work w;
+    w.b = uniform(owner_by_lanes(a.B, (int)i, [&](int b) { return (int)first[b]; }));
+    w.cu = uniform(clamped_cu(a, w.b));
+    w.n_rows = (uniform(clamped_cu(a, w.b + 1)) - w.cu) * a.G;
+    w.start = uniform(a.start[w.b]);
+    w.len = uniform(clamped_len(a, w.b));
+    uint32_t k = i - uniform(first[w.b]);
+    w.kvh = k % a.Hkv;
+    k /= a.Hkv;
+    const int n = pieces(a, w.len);
+    const uint32_t tiles = max(1, (w.n_rows + RT - 1) / RT);
+    w.row0 = k % tiles * RT;
+    w.split = k / tiles;
+    if (w.n_rows <= 0 || (unsigned)w.split >= (unsigned)n) continue;  // cu that does not ascend
+    const int each = piece_keys(w.len, n);
+    w.k0 = w.split * each;
+    w.k1 = min(w.len, w.k0 + each);
+    attend_rows<HD, RB>(a, w, sh);
   }
 }
 
 template <int HD, int RB>
-__global__ __launch_bounds__(256, 2) void k_cache_attend_tile(CacheAttnArgs a) {
+__device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& w, unsigned char* lds) {
   constexpr int RT = 64 * RB, NK = HD / 32, ND = HD / 16, KT = 64;
   constexpr int GB = 32 * HD * 2;             // bytes of K (or V) of a 32-key group
   constexpr int STAGE = 4 * GB;               // two groups of K, then two of V
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * STAGE];
   typedef __attribute__((address_space(3))) void* lds_ptr_t;
   typedef const __attribute__((address_space(1))) void* global_ptr_t;
-  Work w;
-  if (!work_of<RT>(a, w)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, r16 = lane & 15;
 
@@ -390,27 +516,27 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_tile(CacheAttnArgs a) {
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[rb][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int64_t head_elems = (int64_t)HD << a.shift;
-  PageList pl{a.table + (int64_t)w.b * a.max_pages, a.shift - 5, a.n_pages, a.max_pages, 0, 0};
-  const int gmask = (1 << (a.shift - 5)) - 1;
-  // wavefront w loads half (w & 1) of group (w >> 1) of the tile, K and V: HD / 32 blocks each
+  const Groups<HD> groups(a, w);
+  // wavefront w loads half (w & 1) of group (w >> 1) of the tile, K and V: HD / 32 blocks each; the
+  // entry of the tile after is read meanwhile
+  const int last_grp = max((w.len + 31) / 32 - 1, 0);
+  int entry = t0 < t1 ? groups.entry(min(2 * t0 + (wave >> 1), last_grp)) : 0;
   auto fetch = [&](int t, int buf) {
     const int grp = 2 * t + (wave >> 1);
-    if (grp * 32 >= w.len) return;
-    const int64_t e = ((int64_t)pl.page(grp) * a.Hkv + w.kvh) * head_elems + (int64_t)(grp & gmask) * (32 * HD) +
-                      (wave & 1) * (16 * HD) + lane * 8;
+    const int64_t at = groups.offset(entry, grp) + (wave & 1) * (16 * HD * 2);
+    entry = groups.entry(min(grp + 2, last_grp));
+    if (grp > last_grp) return;
+    const char* k = reinterpret_cast<const char*>(a.k) + at + lane * 16;
+    const char* v = reinterpret_cast<const char*>(a.v) + at + lane * 16;
     unsigned char* dst = lds + buf * STAGE + wave * (GB / 2);
 #pragma unroll
     for (int i = 0; i < NK; ++i)
-      __builtin_amdgcn_global_load_lds((global_ptr_t)(a.k + e + i * 512), (lds_ptr_t)(dst + i * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_ptr_t)(k + i * 1024), (lds_ptr_t)(dst + i * 1024), 16, 0, 0);
 #pragma unroll
     for (int i = 0; i < NK; ++i)
-      __builtin_amdgcn_global_load_lds((global_ptr_t)(a.v + e + i * 512), (lds_ptr_t)(dst + 2 * GB + i * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_ptr_t)(v + i * 1024), (lds_ptr_t)(dst + 2 * GB + i * 1024), 16, 0, 0);
   };
-  if (t0 < t1) {
-    pl.load((2 * t0) >> pl.shift5);
-    fetch(t0, 0);
-  }
+  if (t0 < t1) fetch(t0, 0);
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1, key0 = t * KT;
     // tile t has landed, and every wavefront is done with the stage that tile t + 1 goes to
@@ -474,30 +600,18 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_tile(CacheAttnArgs a) {
     }
   }
 
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    float s = l[rb];
-    s += __shfl_xor(s, 16, 64);
-    s += __shfl_xor(s, 32, 64);
-    const int row = w.row0 + (wave * RB + rb) * 16 + r16;
-    if (row >= w.n_rows) continue;
-    const int token = w.cu + row / a.G, head = w.kvh * a.G + row % a.G;
-    if (a.splits == 1) {
-      const float inv = s == 0.f ? 0.f : 1.0f / s;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-        *reinterpret_cast<u32x2_t*>(a.out + out_index(a, token, head, d * 16 + g * 4, HD)) =
-            u32x2_t{pack_bf16x2(o[rb][d][0] * inv, o[rb][d][1] * inv), pack_bf16x2(o[rb][d][2] * inv, o[rb][d][3] * inv)};
-    } else {
-      const int64_t p = ((int64_t)token * a.H + head) * a.splits + w.split;
-      if (g == 0) {
-        a.part_ml[2 * p] = m_ref[rb];
-        a.part_ml[2 * p + 1] = s;
-      }
-#pragma unroll
-      for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4_t*>(a.part_o + p * HD + d * 16 + g * 4) = o[rb][d];
-    }
-  }
+  store_rows<HD, RB>(a, w, wave * RB * 16, m_ref, l, o);
+}
+
+template <int HD, int RB>
+__global__ __launch_bounds__(256, 2) void k_cache_attend_tile(CacheAttnArgs a) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * 4 * 32 * HD * 2];
+  Work w;
+  if (!first_tile<64 * RB>(a, w)) return;
+  do {
+    attend_tile<HD, RB>(a, w, lds);
+    __syncthreads();  // the LDS is free again
+  } while (next_tile<64 * RB>(a, w));
 }
 
 // One wavefront per (row, head): the key ranges' partial results, in their order.
@@ -509,19 +623,25 @@ __global__ __launch_bounds__(256) void k_cache_attend_merge(CacheAttnArgs a) {
   const int token = (int)(i / a.H), head = (int)(i % a.H);
   if (token >= clamped_cu(a, a.B)) return;
   const int b = owner_by_lanes(a.B, token, [&](int x) { return clamped_cu(a, x); });
-  const int len = min(max(a.len[b], 0), a.max_pages << a.shift);
-  const int used = min(a.splits, max(1, (len + a.chunk - 1) / a.chunk));
+  const int len = clamped_len(a, b);
+  const int used = pieces(a, len);
+  if (used == 1) return;  // written already
   const int64_t p = i * a.splits;
-  float m = -INFINITY;
-  for (int s = 0; s < used; ++s) m = fmaxf(m, a.part_ml[2 * (p + s)]);
-  float sum = 0.f, x[E] = {};
-  for (int s = 0; s < used; ++s) {
-    const float ms = a.part_ml[2 * (p + s)], ls = a.part_ml[2 * (p + s) + 1];
-    if (ms == -INFINITY && ls == 0.f) continue;  // no key of this range was seen
-    const float c = ms == -INFINITY ? 1.f : fast_exp2(ms - m);
-    sum += ls * c;
+  // a lane holds one range's maximum and sum; E x 4 B of a lane's O a range
+  const bool has = lane < used;  // no more than 64
+  const float ml = has ? a.part_ml[2 * (p + lane)] : -INFINITY, l = has ? a.part_ml[2 * (p + lane) + 1] : 0.f;
+  float m = ml;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] += a.part_o[(p + s) * HD + lane * E + e] * c;
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float c = ml == m ? 1.f : fast_exp2(ml - m);  // a range without a key is (-inf, 0, 0)
+  float sum = l * c, x[E] = {};
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+#pragma unroll 8
+  for (int s = 0; s < used; ++s) {
+    const float cs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c), s));
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] += a.part_o[(p + s) * HD + lane * E + e] * cs;
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   uint16_t* out = a.out + out_index(a, token, head, lane * E, HD);
@@ -535,16 +655,33 @@ CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int 
   const int64_t most_rows = (int64_t)std::max(1, max_count) * G;
   CacheAttnPlan p{};
   p.tile_rows = most_rows <= 16 ? 16 : (most_rows <= 32 ? 32 : (most_rows <= 64 ? 64 : 128));
-  p.tiles = (int)((int64_t)rows * G / p.tile_rows) + B;
+  p.tiles = (int)((int64_t)rows * G / p.tile_rows) + B;  // no fewer than there are
+  const int64_t each = (most_rows + p.tile_rows - 1) / p.tile_rows;
+  if (p.tile_rows > 32 && each * B <= p.tiles) {
+    p.per_request = (int)each;
+    p.tiles = (int)each * B;
+  }
   const int64_t units = (int64_t)p.tiles * Hkv;
-  const int64_t want = p.tile_rows <= 32 ? 8 * (int64_t)num_cus : 2 * (int64_t)num_cus;
-  const int64_t by_fill = std::max<int64_t>(1, want / std::max<int64_t>(1, units));
-  const int64_t by_len = std::max(1, max_len / 256);
+  if (p.tile_rows <= 32) {
+    // Requests of up to 1.25 ranges stay whole.  1280 keys where the units (tiles and kv heads) could
+    // fill the card whole, 640 where they could not: 64 ragged tokens of 4 kv heads up to 8192 long
+    // 46 us (640: 49, 2048: 54, whole: 117); 32 blocks of 8 kv heads up to 1280 long 22.6 us whole and
+    // 28 in two; 16 tokens of 8 kv heads up to 4096 long 18.9 us at 768, 21.8 at 1280; one token of 4
+    // kv heads, 8192 long, 18.5 and 21.2.  No more than 32 ranges unless the units are very few: each
+    // is written and read once more (one token of 8 kv heads, 32768 long: 30 us in 32 ranges, 34 in 64).
+    const int keys = units >= num_cus ? 1280 : 640;
+    const int64_t cap = std::min<int64_t>(64, std::max<int64_t>(32, num_cus / units));
+    const int64_t n = max_len <= keys + keys / 4 ? 1 : (max_len + (int64_t)keys - 1) / keys;
+    p.splits = (int)std::min(n, cap);
+  } else {
+    const int64_t want = std::max<int64_t>(1, 2 * (int64_t)num_cus / units), by_len = std::max(1, max_len / 256);
+    p.splits = (int)std::min<int64_t>(std::min(want, by_len), 64);
+  }
   const size_t per_split = (size_t)std::max(1, rows) * H * (2 + hd);
-  p.splits = (int)std::min<int64_t>(std::min(by_fill, by_len), 64);
-  p.splits = (int)std::max<size_t>(1, std::min<size_t>(p.splits, most_ws_floats / per_split));
-  p.chunk = ((max_len + p.splits - 1) / p.splits + 63) / 64 * 64;
-  if (p.chunk < 64) p.chunk = 64;
+  const int64_t most = std::min<int64_t>(most_ws_floats / per_split, 0x7fffffffLL / units);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, most));
+  p.chunk = std::max(64, ((max_len + p.splits - 1) / p.splits + 63) / 64 * 64);
+  p.workgroups = (int)std::min<int64_t>(6 * num_cus, units * p.splits);
   p.ws_floats = p.splits > 1 ? per_split * p.splits : 0;
   return p;
 }
@@ -553,6 +690,7 @@ hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnPlan& p, int h
   if (a.rows == 0) return hipSuccess;
   a.G = a.H / a.Hkv;
   a.tiles = p.tiles;
+  a.per_request = p.per_request;
   a.splits = p.splits;
   a.chunk = p.chunk;
   if (p.splits > 1 && !ws) return hipErrorInvalidValue;
@@ -560,11 +698,12 @@ hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnPlan& p, int h
   a.part_ml = ws ? ws + (size_t)a.rows * a.H * p.splits * hd : nullptr;
   const int64_t wgs = (int64_t)p.tiles * p.splits * a.Hkv;
   if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs);
+  const dim3 grid((unsigned)wgs), few((unsigned)p.workgroups);
+  const size_t lds = (size_t)(a.B + 1) * 4;
 #define ATTEND(HD_)                                                                                              \
   do {                                                                                                           \
-    if (p.tile_rows == 16) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 1>), grid, dim3(256), 0, s, a);          \
-    else if (p.tile_rows == 32) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 2>), grid, dim3(256), 0, s, a);     \
+    if (p.tile_rows == 16) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 1>), few, dim3(256), lds, s, a);         \
+    else if (p.tile_rows == 32) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 2>), few, dim3(256), lds, s, a);    \
     else if (p.tile_rows == 64) hipLaunchKernelGGL((k_cache_attend_tile<HD_, 1>), grid, dim3(256), 0, s, a);     \
     else hipLaunchKernelGGL((k_cache_attend_tile<HD_, 2>), grid, dim3(256), 0, s, a);                            \
     if (p.splits > 1) {                                                                                          \

@@ -251,13 +251,15 @@ struct CacheAttnArgs {
   float *part_o, *part_ml;  // [rows][H][splits][hd], [rows][H][splits][2]
   int B, rows, H, Hkv, shift, n_pages, max_pages, causal, panels;
   float scale_log2;
-  int G, tiles, splits, chunk;  // set from the plan
+  int G, tiles, per_request, splits, chunk;  // set from the plan
 };
 // tile_rows (token, head) rows a workgroup, `splits` ranges of `chunk` keys (the last takes the
 // rest).  Made from sizes a caller keeps from call to call, never from the lengths on the device,
 // so that a row's sums do not depend on what else is in the batch.
 struct CacheAttnPlan {
   int tile_rows, tiles, splits, chunk;
+  int per_request;  // tiles of each request where they have about as many rows, or 0
+  int workgroups;   // of the few-rows kernel
   size_t ws_floats;
 };
 CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int max_count, int max_len,
