@@ -19,6 +19,7 @@
 // Either runs over key ranges where the rows alone would not fill the card; the ranges' (max, sum, O)
 // go to the workspace and k_cache_attend_merge folds them in order.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "internal.hpp"
@@ -67,8 +68,9 @@ struct Work {
 // The first tile of a workgroup of k_cache_attend_tile; false when it has none.  Workgroups are
 // numbered with the key range slowest and from the last one on: what only long requests have starts
 // first, and the first range, which holds the short ones whole, fills the gaps at the end.  With
-// `per_request` tiles a request (every request has about as many rows) the request follows from the
-// number, the kv head the fastest.  Else (a prompt beside single tokens) tile t belongs to the request
+// `per_request` tiles a request (every request has about as many rows) a workgroup's place follows from
+// its number, the kv head the fastest and the later tiles, which see more keys under the causal mask,
+// before the earlier ones (382 us against 402).  Else (a prompt beside single tokens) tile t belongs to the request
 // b with base_b <= t < base_(b+1), base_b = cu_b G / RT + b, which leaves each request at least as many
 // tiles as it fills and needs no pass over the lengths, and an XCD takes a range of kv heads and tiles,
 // whose keys its L2 then holds.
@@ -78,15 +80,15 @@ __device__ __forceinline__ bool first_tile(const CacheAttnArgs& a, Work& w) {
   if (a.per_request > 0) {
     w.kvh = li % a.Hkv;
     li /= a.Hkv;
-    w.row0 = li % a.per_request * RT;
-    li /= a.per_request;
     w.b = li % a.B;
-    w.split = a.splits - 1 - li / a.B;
+    li /= a.B;
+    w.row0 = (a.per_request - 1 - li % a.per_request) * RT;
+    w.split = a.splits - 1 - li / a.per_request;
   } else {
     const int n = a.tiles * a.Hkv;
     w.split = a.splits - 1 - li / n;
     li = xcd_remap(li % n, n);
-    const int t = a.tiles - 1 - li % a.tiles;  // later tiles see more keys under the causal mask: they start first
+    const int t = a.tiles - 1 - li % a.tiles;  // later tiles first here too
     w.kvh = li / a.tiles;
     w.b = uniform(owner_by_lanes(a.B, t, [&](int b) { return (int)((int64_t)clamped_cu(a, b) * a.G / RT) + b; }));
     w.row0 = (t - (int)((int64_t)uniform(clamped_cu(a, w.b)) * a.G / RT) - w.b) * RT;
@@ -148,36 +150,47 @@ __device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Work& w, in
     qf[kk] = as_bf16x8(row < w.n_rows ? *reinterpret_cast<const u32x4_t*>(q + kk * 32) : u32x4_t{0, 0, 0, 0});
 }
 
-// Moves the reference of the scores st[NB] of one query (max over its four lane groups) and
-// rescales, then turns the scores into terms.
-template <int NB, int ND>
-__device__ __forceinline__ void soften(f32x4_t (&st)[NB], float scale_log2, float& m_ref, float& m_use, float& l,
-                                       f32x4_t (&o)[ND]) {
-  float lmax = -INFINITY;
+// Moves the reference of the scores st[rb] of a query (the maximum over its four lane groups) and
+// rescales, where one of them needs it, then turns the scores into terms.
+template <int RB, int NB, int ND>
+__device__ __forceinline__ void soften(f32x4_t (&st)[RB][NB], float scale_log2, float (&m_ref)[RB], float (&m_use)[RB],
+                                       float (&l)[RB], f32x4_t (&o)[RB][ND]) {
+  float lmax[RB];
+  bool moves = false;
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
+  for (int rb = 0; rb < RB; ++rb) {
+    lmax[rb] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lmax = fmaxf(lmax, st[kb][i]);
-  if (__any(lmax * scale_log2 > m_ref + SLACK)) {
-    float tmax = fmaxf(lmax, __shfl_xor(lmax, 16, 64));
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-    const float tm = tmax * scale_log2;
-    if (tm > m_ref + SLACK) {  // never while no key was seen and none is
-      const float alpha = fast_exp2(m_ref - tm);
-      m_ref = m_use = tm;
-      l *= alpha;
+    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-      for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      for (int i = 0; i < 4; ++i) lmax[rb] = fmaxf(lmax[rb], st[rb][kb][i]);
+    moves |= lmax[rb] * scale_log2 > m_ref[rb] + SLACK;
+  }
+  if (__any(moves)) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float tmax = fmaxf(lmax[rb], __shfl_xor(lmax[rb], 16, 64));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+      const float tm = tmax * scale_log2;
+      if (tm > m_ref[rb] + SLACK) {  // never while no key was seen and none is
+        const float alpha = fast_exp2(m_ref[rb] - tm);
+        m_ref[rb] = m_use[rb] = tm;
+        l[rb] *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[rb][d] *= alpha;
+      }
     }
   }
 #pragma unroll
-  for (int kb = 0; kb < NB; ++kb)
+  for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float p = fast_exp2(fmaf(st[kb][i], scale_log2, -m_use));  // m_use 0 until a key is seen
-      st[kb][i] = p;
-      l += p;
-    }
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = fast_exp2(fmaf(st[rb][kb][i], scale_log2, -m_use[rb]));  // m_use 0 until a key is seen
+        st[rb][kb][i] = p;
+        l[rb] += p;
+      }
 }
 
 __device__ __forceinline__ bf16x8_t terms_operand(const f32x4_t& x, const f32x4_t& y) {
@@ -369,8 +382,8 @@ __device__ __forceinline__ void attend_rows(const CacheAttnArgs& a, const Work& 
           for (int i = 0; i < 4; ++i)
             if (4 * kb + i >= n) st[rb][kb][i] = -INFINITY;
       }
-      soften<2, ND>(st[rb], a.scale_log2, m_ref[rb], m_use[rb], l[rb], o[rb]);
     }
+    soften<RB, 2, ND>(st, a.scale_log2, m_ref, m_use, l, o);
     if (grp * 32 + 32 > w.len) {  // slots behind the last key may hold anything
 #pragma unroll
       for (int d = 0; d < ND; ++d) vf[d] = keep_keys(vf[d], w.len - key);
@@ -483,14 +496,23 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
   }
 }
 
+// Bound by the products and, nearly as much, by the LDS reads that feed them (a fragment of K or V
+// serves RB x 16 rows) and the exponentials: 4 x 2048 tokens of 28 heads of 128 behind 2048 others,
+// causal, 344 us, 1.05 PFLOP/s.  Tiles that no row's limit cuts take a path without masks or branches
+// but one, for a moved reference.  Tried at RB = 2: 32-key tiles in 2 to 4 stages, two or three
+// workgroups a CU (366 us); RB = 3 (348 us, and 54 against 44 us where 2 x 1024 tokens of 32 heads
+// leave fewer workgroups than places); RB = 4 on one wavefront a SIMD (544 us).
+constexpr int TILE_KEYS = 64, TILE_STAGES = 2;
+
 template <int HD, int RB>
 __device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& w, unsigned char* lds) {
-  constexpr int RT = 64 * RB, NK = HD / 32, ND = HD / 16, KT = 64;
-  constexpr int GB = 32 * HD * 2;             // bytes of K (or V) of a 32-key group
-  constexpr int STAGE = 4 * GB;               // two groups of K, then two of V
+  constexpr int RT = 64 * RB, NK = HD / 32, ND = HD / 16, KT = TILE_KEYS, NS = TILE_STAGES;
+  constexpr int GB = 32 * HD * 2;           // bytes of K (or V) of a 32-key group
+  constexpr int NG = KT / 32, VAT = NG * GB, STAGE = 2 * NG * GB;  // a stage: groups of K, then of V
+  constexpr int NL = NG * ND / 4;           // blocks of K (and of V) that a wavefront loads
   typedef __attribute__((address_space(3))) void* lds_ptr_t;
   typedef const __attribute__((address_space(1))) void* global_ptr_t;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int g = lane >> 4, r16 = lane & 15;
 
   bf16x8_t qf[RB][NK];
@@ -501,9 +523,11 @@ __device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& 
     load_q<HD>(a, w, row, qf[rb]);
     lim[rb] = min(limit_of(a, w, row), w.k1);
   }
-  // keys that some row of the wavefront sees, and that some row of the workgroup does
-  const int last = min(w.row0 + (wave + 1) * RB * 16, w.n_rows) - 1;
-  const int wave_end = w.row0 + wave * RB * 16 < w.n_rows ? min(w.k1, limit_of(a, w, last)) : 0;
+  // keys that every row of the wavefront sees, that some row of it does, and that some row of the
+  // workgroup does
+  const int first = w.row0 + wave * RB * 16, last = min(first + RB * 16, w.n_rows) - 1;
+  const int wave_full = first < w.n_rows ? min(w.k1, limit_of(a, w, first)) : 0;
+  const int wave_end = first < w.n_rows ? min(w.k1, limit_of(a, w, last)) : 0;
   const int end = min(w.k1, limit_of(a, w, min(w.row0 + RT, w.n_rows) - 1));
   const int t0 = w.k0 / KT, t1 = (end + KT - 1) / KT;
 
@@ -517,38 +541,32 @@ __device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& 
     for (int d = 0; d < ND; ++d) o[rb][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   const Groups<HD> groups(a, w);
-  // wavefront w loads half (w & 1) of group (w >> 1) of the tile, K and V: HD / 32 blocks each; the
-  // entry of the tile after is read meanwhile
-  const int last_grp = max((w.len + 31) / 32 - 1, 0);
-  int entry = t0 < t1 ? groups.entry(min(2 * t0 + (wave >> 1), last_grp)) : 0;
+  // A wavefront loads its share of a tile's blocks; the entry of the tile after is read meanwhile.
+  // Behind the last key the last group is loaded once more, so that each tile counts the same loads.
+  const int last_grp = max((w.len + 31) / 32 - 1, 0), sub = wave * NG / 4, part = wave - sub * (4 / NG);
+  int entry = t0 < t1 ? groups.entry(min(NG * t0 + sub, last_grp)) : 0;
   auto fetch = [&](int t, int buf) {
-    const int grp = 2 * t + (wave >> 1);
-    const int64_t at = groups.offset(entry, grp) + (wave & 1) * (16 * HD * 2);
-    entry = groups.entry(min(grp + 2, last_grp));
-    if (grp > last_grp) return;
+    const int grp = min(NG * t + sub, last_grp);
+    const int64_t at = groups.offset(entry, grp) + part * (NL * 1024);
+    entry = groups.entry(min(NG * (t + 1) + sub, last_grp));
     const char* k = reinterpret_cast<const char*>(a.k) + at + lane * 16;
     const char* v = reinterpret_cast<const char*>(a.v) + at + lane * 16;
-    unsigned char* dst = lds + buf * STAGE + wave * (GB / 2);
+    unsigned char* dst = lds + buf * STAGE + wave * (NL * 1024);
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
+    for (int i = 0; i < NL; ++i)
       __builtin_amdgcn_global_load_lds((global_ptr_t)(k + i * 1024), (lds_ptr_t)(dst + i * 1024), 16, 0, 0);
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
-      __builtin_amdgcn_global_load_lds((global_ptr_t)(v + i * 1024), (lds_ptr_t)(dst + 2 * GB + i * 1024), 16, 0, 0);
+    for (int i = 0; i < NL; ++i)
+      __builtin_amdgcn_global_load_lds((global_ptr_t)(v + i * 1024), (lds_ptr_t)(dst + VAT + i * 1024), 16, 0, 0);
   };
-  if (t0 < t1) fetch(t0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1, key0 = t * KT;
-    // tile t has landed, and every wavefront is done with the stage that tile t + 1 goes to
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t + 1 < t1) fetch(t + 1, buf ^ 1);
-    if (key0 >= wave_end) continue;
-    const unsigned char* kl = lds + buf * STAGE + lane * 16;
-    const unsigned char* vl = kl + 2 * GB;
-    f32x4_t st[RB][4];
+  auto fold = [&](const unsigned char* stage, int key0, auto edge) {
+    constexpr bool EDGE = decltype(edge)::value;
+    const unsigned char *kl = stage + lane * 16, *vl = kl + VAT;
+    // the scheduler's strategy 1 mixes LDS reads and products best: 344 us against 354 (0 and 2: 348, 357)
+    __builtin_amdgcn_iglp_opt(1);
+    f32x4_t st[RB][2 * NG];
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
+    for (int kb = 0; kb < 2 * NG; ++kb) {
       bf16x8_t kf[NK];
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) kf[kk] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(kl + (kb * NK + kk) * 1024));
@@ -560,24 +578,20 @@ __device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& 
           st[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk], qf[rb][kk], st[rb][kb], 0, 0, 0);
       }
     }
-    bool cut = false;  // some row's last key lies in the tile
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const int n = lim[rb] - key0 - 8 * g;  // the lane's terms are keys 32 (kb / 2) + 4 (kb % 2) + i
-      if (__any(n < 40)) {
-        cut = true;
+      if constexpr (EDGE) {
+        const int n = lim[rb] - key0 - 8 * g;  // the lane's terms are keys 32 (kb / 2) + 4 (kb % 2) + i
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
+        for (int kb = 0; kb < 2 * NG; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (32 * (kb >> 1) + 4 * (kb & 1) + i >= n) st[rb][kb][i] = -INFINITY;
       }
-      soften<4, ND>(st[rb], a.scale_log2, m_ref[rb], m_use[rb], l[rb], o[rb]);
     }
-    const bool ragged = key0 + KT > w.len;  // slots behind the last key may hold anything
-    cut = cut && a.causal;
+    soften<RB, 2 * NG, ND>(st, a.scale_log2, m_ref, m_use, l, o);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int ks = 0; ks < NG; ++ks) {
       bool bad = false;
       bf16x8_t p[RB];
 #pragma unroll
@@ -585,27 +599,48 @@ __device__ __forceinline__ void attend_tile(const CacheAttnArgs& a, const Work& 
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         u32x4_t v = *reinterpret_cast<const u32x4_t*>(vl + (ks * ND + d) * 1024);
-        if (ragged) v = keep_keys(v, w.len - key0 - 32 * ks - 8 * g);
-        if (cut) v = finite_only(v, bad);
+        if constexpr (EDGE) {  // slots behind the last key may hold anything
+          v = keep_keys(v, w.len - key0 - 32 * ks - 8 * g);
+          if (a.causal) v = finite_only(v, bad);
+        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
           o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), p[rb], o[rb][d], 0, 0, 0);
       }
-      if (__any(bad)) {
+      if constexpr (EDGE) {
+        if (__any(bad)) {
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          add_non_finite<ND>(reinterpret_cast<const uint16_t*>(lds + buf * STAGE + 2 * GB + ks * GB), st[rb][2 * ks],
-                             st[rb][2 * ks + 1], lim[rb] - key0 - 32 * ks, o[rb]);
+          for (int rb = 0; rb < RB; ++rb)
+            add_non_finite<ND>(reinterpret_cast<const uint16_t*>(stage + VAT + ks * GB), st[rb][2 * ks],
+                               st[rb][2 * ks + 1], min(lim[rb], w.k1) - key0 - 32 * ks, o[rb]);
+        }
       }
     }
+  };
+  if (t0 < t1) {
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) fetch(t0 + i, i);
   }
+  int buf = 0;
+  for (int t = t0; t < t1; ++t) {
+    // tile t has landed, and every wavefront is done with the stage that tile t + NS - 1 goes to
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * 2 * NL) : "memory");
+    __syncthreads();
+    fetch(t + NS - 1, buf ? buf - 1 : NS - 1);
+    if (t * KT < wave_end) {
+      if (t * KT + KT <= wave_full) fold(lds + buf * STAGE, t * KT, std::false_type{});
+      else fold(lds + buf * STAGE, t * KT, std::true_type{});
+    }
+    buf = buf + 1 < NS ? buf + 1 : 0;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads behind the last tile
 
   store_rows<HD, RB>(a, w, wave * RB * 16, m_ref, l, o);
 }
 
 template <int HD, int RB>
 __global__ __launch_bounds__(256, 2) void k_cache_attend_tile(CacheAttnArgs a) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * 4 * 32 * HD * 2];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[TILE_STAGES * TILE_KEYS * HD * 4];
   Work w;
   if (!first_tile<64 * RB>(a, w)) return;
   do {
