@@ -497,6 +497,8 @@ def cache_attention(cache: KVCache, layer, q, chunk: Chunk, max_count=0, max_len
         key = (n_heads, rows, max_count, max_len)
         n = cache._workspaces.get(key)
         if n is None:
+            if len(cache._workspaces) >= 256:  # a max_len that grows with every call
+                cache._workspaces.clear()
             n = cache._workspaces[key] = cache_attention_workspace(cache, n_heads, chunk, max_count, max_len)
         if n:
             workspace = _empty(n, torch.uint8, q.device, stream)

@@ -27,6 +27,12 @@
 // 65536 bf16 numbers in eight windows of 32-bit counts, at one reading of the row each; finite
 // numbers far below the maximum (a ban by bf16's lowest one), whose terms are 0 in 64 bits, do not
 // count.
+//
+// 4096 rows of 126464 take 229 us, 4.5 TB/s.  Three things of like size share that time: the row's
+// bytes (150 us at the 6.9 TB/s of a plain reading), the LDS adds (117 us: 3.7 ns a wavefront's 64
+// on a CU when they fall on some 500 words, 1.8 without bank conflicts) and about 7 instructions a
+// logit (95 us).  Steps 2 to 4 are 17 of a row's 38 us, beside two other rows' counting.  A single
+// row is bound by latency: 2048 logits 8 us in the kernel, 126464 17 us, 9 of them counting.
 #include <limits.h>
 
 #include <algorithm>
@@ -879,7 +885,8 @@ hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   // Up to a row per CU: 1024 threads, 32 x 126464 in 21.9 us against 25.0 with 512.  More: 512, three
   // rows to a CU, 4096 x 126464 in 253 us against 378 with 1024 and one, 303 with 1024 in 64 registers
-  // and two, 310 with 512 in 64 registers and four (both spill); 777 x 50257 in 41.5 against 57, 54, 47.
+  // and two, 310 with 512 in 64 registers and four (both spill); 777 x 50257 in 41.5 against 57, 54, 47
+  // (today's 229 and 39.3 us with the sums' entries side by side).
   const bool many = a.rows > 256;
   if (many) hipLaunchKernelGGL((k_vocab_sample<512, true>), dim3(a.rows), dim3(512), 0, s, a);
   else hipLaunchKernelGGL((k_vocab_sample<1024, false>), dim3(a.rows), dim3(1024), 0, s, a);

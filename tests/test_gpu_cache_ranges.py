@@ -62,6 +62,17 @@ def test_attention_requests_without_rows():
         assert (out == 9).all()
 
 
+def test_attention_expected_lengths_that_grow():
+    """A max_len of its own for every call: the sizes kept on the host stay few, results the same."""
+    require_gpu()
+    rng = np.random.default_rng(4)
+    cache, chunk, q, ks, vs, T = requests(rng, [300, 40], [1, 1], 64, 4, 2, 64)
+    want = cache_attention(cache, 0, q, chunk, max_count=1, max_len=1)
+    for n in range(2, 600):
+        got = cache_attention(cache, 0, q, chunk, max_count=1, max_len=n)
+    assert torch.equal(got, want) and len(cache._workspaces) <= 256
+
+
 @pytest.mark.parametrize("H,Hkv", [(9, 3), (13, 13)])
 @pytest.mark.parametrize("f32", [False, True])
 def test_store_large(H, Hkv, f32):
