@@ -446,6 +446,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
   constexpr int RT = RB * 16;
   extern __shared__ uint32_t first[];  // [B + 1]: pieces of the requests before
   __shared__ uint32_t part[4];
+  __shared__ int near[4][256];  // cu, rows, start and len of the first requests, read once
   __shared__ RowsShared<HD, RB> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   uint32_t carry = 0;
@@ -453,16 +454,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
     const int b = b0 + tid;
     uint32_t n = 0;
     if (b < a.B) {
-      const int rows = (clamped_cu(a, b + 1) - clamped_cu(a, b)) * a.G, len = clamped_len(a, b);
+      const int cu = clamped_cu(a, b), rows = (clamped_cu(a, b + 1) - cu) * a.G, len = clamped_len(a, b);
+      if (b0 == 0) {
+        near[0][tid] = cu;
+        near[1][tid] = rows;
+        near[2][tid] = a.start[b];
+        near[3][tid] = len;
+      }
       if (rows > 0)
         n = (uint32_t)((rows + RT - 1) / RT) * (uint32_t)a.Hkv * (uint32_t)pieces(a, len);
     }
-    uint32_t s = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t u = __shfl_up(s, o, 64);
-      if (lane >= o) s += u;
-    }
+    uint32_t s = wave_scan(n);
     if (lane == 63) part[wave] = s;
     __syncthreads();
 #pragma unroll
@@ -477,10 +479,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
   for (uint32_t i = blockIdx.x; i < total; i += gridDim.x) {
     Work w;
     w.b = uniform(owner_by_lanes(a.B, (int)i, [&](int b) { return (int)first[b]; }));
-    w.cu = uniform(clamped_cu(a, w.b));
-    w.n_rows = (uniform(clamped_cu(a, w.b + 1)) - w.cu) * a.G;
-    w.start = uniform(a.start[w.b]);
-    w.len = uniform(clamped_len(a, w.b));
+    if (w.b < 256) {
+      w.cu = uniform(near[0][w.b]);
+      w.n_rows = uniform(near[1][w.b]);
+      w.start = uniform(near[2][w.b]);
+      w.len = uniform(near[3][w.b]);
+    } else {
+      w.cu = uniform(clamped_cu(a, w.b));
+      w.n_rows = (uniform(clamped_cu(a, w.b + 1)) - w.cu) * a.G;
+      w.start = uniform(a.start[w.b]);
+      w.len = uniform(clamped_len(a, w.b));
+    }
     uint32_t k = i - uniform(first[w.b]);
     w.kvh = k % a.Hkv;
     k /= a.Hkv;

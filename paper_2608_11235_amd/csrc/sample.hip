@@ -131,28 +131,6 @@ struct Shared {
   uint32_t first_id;
 };
 
-// ---- wavefront sums by lane moves (DPP) -----------------------------------------------------
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t v) {  // 0 where a lane has no source
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double moved(double v) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = moved<CTRL, ROWS>((uint32_t)b), hi = moved<CTRL, ROWS>((uint32_t)(b >> 32));
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// inclusive sums over the lanes: inside rows of 16, then the rows before
-template <class T>
-__device__ __forceinline__ T scan(T v) {
-  v += moved<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
-  v += moved<0x112, 0xf>(v);
-  v += moved<0x114, 0xf>(v);
-  v += moved<0x118, 0xf>(v);
-  v += moved<0x142, 0xa>(v);  // row_bcast 15, 31
-  v += moved<0x143, 0xc>(v);
-  return v;
-}
 __device__ __forceinline__ uint32_t lane_value(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
 __device__ __forceinline__ double lane_value(double v, int l) {
   const uint64_t b = __builtin_bit_cast(uint64_t, v);
@@ -401,8 +379,8 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < 4; ++j) st += c[j] ? c[j] * w[j] : 0.0;
       }
-      st = lane_value(scan(st), 63);
-      s1 = lane_value(scan(s1), 63);
+      st = lane_value(wave_scan(st), 63);
+      s1 = lane_value(wave_scan(s1), 63);
       if (lane == 0) {
         sh.wt[win * NENT + e] = st;
         sh.w1[win * NENT + e] = s1;
@@ -468,9 +446,9 @@ struct Row {
       s += sh.wt[lane * EPL + i];
       s1 += sh.w1[lane * EPL + i];
     }
-    ni = scan(n);
-    si = scan(s);
-    return lane_value(scan(s1), 63);
+    ni = wave_scan(n);
+    si = wave_scan(s);
+    return lane_value(wave_scan(s1), 63);
   }
 
   // the first lane of a border, or, where rounding left the last sum short of it, the last lane in use
@@ -528,8 +506,8 @@ struct Row {
     uint32_t cn;
     double cs, w[4];
     const u32x4_t c = four(e, w, cn, cs);
-    const uint32_t bi = scan(cn) + before;
-    const double mi = scan(cs) + mass;
+    const uint32_t bi = wave_scan(cn) + before;
+    const double mi = wave_scan(cs) + mass;
     l = border(cn > 0 && past(bi, mi), cn > 0);
     Place p{0, bi - cn, 0, mi - cs, 0.0};
     bool found = false;
@@ -570,8 +548,8 @@ struct Row {
         cn += c[j];
         cs += c[j] * w[j];
       }
-    mass = lane_value(scan(cs), 63);
-    return lane_value(scan(cn), 63);
+    mass = lane_value(wave_scan(cs), 63);
+    return lane_value(wave_scan(cn), 63);
   }
 };
 
@@ -689,12 +667,12 @@ __device__ __forceinline__ void find_id(Sh& sh, const uint16_t* x, int V, int ma
     for (int k = 0; k < 4; ++k) {
       own[k] = __popc(hits[k]);
       inc[k] = 0;
-      if (__any(hits[k] != 0)) inc[k] = scan(own[k]);
+      if (__any(hits[k] != 0)) inc[k] = wave_scan(own[k]);
       if (lane == 63) sh.tot[i & 1][k * NW + wave] = inc[k];
     }
     __syncthreads();
     static_assert(4 * NW <= 64, "a total of each wavefront and chunk to a lane");
-    const uint32_t all = scan(lane < 4 * NW ? sh.tot[i & 1][lane] : 0u), total = lane_value(all, 63);
+    const uint32_t all = wave_scan(lane < 4 * NW ? sh.tot[i & 1][lane] : 0u), total = lane_value(all, 63);
     if (left < seen + total) {
       const uint32_t at = back ? total - 1 - (left - seen) : left - seen;
 #pragma unroll
@@ -731,7 +709,7 @@ __device__ __forceinline__ void count_entries(Sh& sh, int win) {
       const int in = c[0] ? 0 : (c[1] ? 1 : (c[2] ? 2 : 3));
       least = lane_value((uint32_t)(i0 + in), __ffsll(used) - 1);
     }
-    const uint32_t total = used ? lane_value(scan(cn), 63) : 0;
+    const uint32_t total = used ? lane_value(wave_scan(cn), 63) : 0;
     if (lane == 0) sh.cnt[win * NENT + e] = total;
   }
   if (lane == 0) sh.first[wave] = least;
@@ -866,7 +844,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 6 : 4) void k_vocab_sample(SampleAr
     __syncthreads();
     if (PAIRED) {  // a count that passed 65535 took 65535 or 65536 off the sum
       static_assert(Bins::ENTRIES == 64, "an entry to a lane");
-      const uint32_t n = lane_value(scan(sh.cnt[tid & 63]), 63);
+      const uint32_t n = lane_value(wave_scan(sh.cnt[tid & 63]), 63);
       if (n + sh.uncounted != (uint32_t)a.V) special = OTHER;
     }
     if (!special) {
