@@ -55,9 +55,9 @@ __device__ __forceinline__ int clamped_len(const CacheAttnArgs& a, int b) { retu
 // Key ranges that a request is attended in, and the keys of each (the last has what is left): they
 // follow from its own length, never from the others in the batch.
 __device__ __forceinline__ int pieces(const CacheAttnArgs& a, int len) {
-  return min(a.splits, max(1, (int)(((int64_t)len + a.chunk - 1) / a.chunk)));
+  return min(a.splits, max(1, (int)(((uint32_t)len + a.chunk - 1) / (uint32_t)a.chunk)));  // neither beyond 2^30
 }
-__device__ __forceinline__ int piece_keys(int len, int n) { return ((len + 31) / 32 + n - 1) / n * 32; }
+__device__ __forceinline__ int piece_keys(int len, int n) { return (int)(((uint32_t)(len + 31) / 32 + n - 1) / (uint32_t)n * 32); }
 
 // What a workgroup works on: rows [row0, row0 + RT) of the (token, head) rows of request b and kv
 // head kvh, keys [k0, k1) of its `len`.
@@ -663,14 +663,22 @@ template <int HD>
 __global__ __launch_bounds__(256) void k_cache_attend_merge(CacheAttnArgs a) {
   constexpr int E = HD / 64;
   const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int token = (int)(i / a.H), head = (int)(i % a.H);
+  const uint32_t i = blockIdx.x * 4 + uniform(threadIdx.x >> 6);  // rows H is no more than 2^30
+  const int token = (int)(i / (uint32_t)a.H), head = (int)(i % (uint32_t)a.H);
   if (token >= clamped_cu(a, a.B)) return;
   const int b = owner_by_lanes(a.B, token, [&](int x) { return clamped_cu(a, x); });
   const int len = clamped_len(a, b);
   const int used = pieces(a, len);
   if (used == 1) return;  // written already
-  const int64_t p = i * a.splits;
+  const int64_t p = (int64_t)i * a.splits;
+  float t[8][E];  // eight ranges' loads at a time
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) t[u][e] = a.part_o[(p + min(s0 + u, used - 1)) * HD + lane * E + e];
+  };
+  load(0);
   // a lane holds one range's maximum and sum; E x 4 B of a lane's O a range
   const bool has = lane < used;  // no more than 64
   const float ml = has ? a.part_ml[2 * (p + lane)] : -INFINITY, l = has ? a.part_ml[2 * (p + lane) + 1] : 0.f;
@@ -681,11 +689,15 @@ __global__ __launch_bounds__(256) void k_cache_attend_merge(CacheAttnArgs a) {
   float sum = l * c, x[E] = {};
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
-#pragma unroll 8
-  for (int s = 0; s < used; ++s) {
-    const float cs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c), s));
+  for (int s0 = 0; s0 < used; s0 += 8) {
+    if (s0 > 0) load(s0);
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] += a.part_o[(p + s) * HD + lane * E + e] * cs;
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= used) continue;
+      const float cs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(c), s0 + u));
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] += t[u][e] * cs;
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   uint16_t* out = a.out + out_index(a, token, head, lane * E, HD);
@@ -708,12 +720,16 @@ CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int 
   const int64_t units = (int64_t)p.tiles * Hkv;
   if (p.tile_rows <= 32) {
     // Requests of up to 1.25 ranges stay whole.  1280 keys where the units (tiles and kv heads) could
-    // fill the card whole, 640 where they could not: 64 ragged tokens of 4 kv heads up to 8192 long
-    // 46 us (640: 49, 2048: 54, whole: 117); 32 blocks of 8 kv heads up to 1280 long 22.6 us whole and
-    // 28 in two; 16 tokens of 8 kv heads up to 4096 long 18.9 us at 768, 21.8 at 1280; one token of 4
-    // kv heads, 8192 long, 18.5 and 21.2.  No more than 32 ranges unless the units are very few: each
-    // is written and read once more (one token of 8 kv heads, 32768 long: 30 us in 32 ranges, 34 in 64).
-    const int keys = units >= num_cus ? 1280 : 640;
+    // fill the card whole, 640 where they could not, 320 where they are very few (heads of 128):
+    //   64 ragged tokens of 4 kv heads up to 8192 long     44 us at 1280, 47 at 640, 50 at 320
+    //   32 blocks of 8 kv heads up to 1280 long            22 us whole, 28 in two
+    //   256 tokens of 8 kv heads up to 1024 long           68 us whole, 72 in two
+    //   16 tokens of 8 kv heads up to 4096 long            21 us at 1280, 18 at 640, 19 at 320
+    //   one token of 4 kv heads, 8192 long                 19 us at 1280, 15 at 640, 14 at 320
+    //   one block of 32 kv heads, 1280 long                18 us whole, 15.6 at 640, 14 at 320
+    // No more than 32 ranges unless the units are very few, since each is written and read once more
+    // (one token of 8 kv heads, 32768 long: 28 us in 32 ranges, 31 in 64).
+    const int keys = units >= num_cus ? 1280 : (8 * units > num_cus ? 640 : 320);
     const int64_t cap = std::min<int64_t>(64, std::max<int64_t>(32, num_cus / units));
     const int64_t n = max_len <= keys + keys / 4 ? 1 : (max_len + (int64_t)keys - 1) / keys;
     p.splits = (int)std::min(n, cap);
