@@ -28,10 +28,10 @@
 // numbers far below the maximum (a ban by bf16's lowest one), whose terms are 0 in 64 bits, do not
 // count.
 //
-// 4096 rows of 126464 take 229 us, 4.5 TB/s.  Three things of like size share that time: the row's
-// bytes (150 us at the 6.9 TB/s of a plain reading), the LDS adds (117 us: 3.7 ns a wavefront's 64
+// 4096 rows of 126464 take 225 us, 4.6 TB/s.  Three things of like size share that time: the rows'
+// bytes (150 us at the 6.9 TB/s of a plain reading, and up to a third more for step 4), the LDS adds (117 us: 3.7 ns a wavefront's 64
 // on a CU when they fall on some 500 words, 1.8 without bank conflicts) and about 7 instructions a
-// logit (95 us).  Steps 2 to 4 are 17 of a row's 38 us, beside two other rows' counting.  A single
+// logit (95 us).  Steps 2 to 4 are 13 of a row's 32 us, beside two other rows' counting.  A single
 // row is bound by latency: 2048 logits 8 us in the kernel, 126464 17 us, 9 of them counting.
 #include <limits.h>
 
@@ -612,31 +612,34 @@ __device__ __forceinline__ void pick(Row<Scheme, NT, Sh>& row, int first, const 
   }
 }
 
-// Step 4: the rank-th id that holds the value, in blocks of 4 NT chunks of eight ids, from the front
-// or from the back, the next block's loads ahead.
+// Step 4: the rank-th id that holds the value, in blocks of CH NT chunks of eight ids, from the front
+// or from the back.
 template <int NT, class Sh>
 __device__ __forceinline__ void find_id(Sh& sh, const uint16_t* x, int V, int mask_id) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  constexpr int NW = NT / 64;
+  constexpr int NW = NT / 64, CH = 2;  // chunks a thread and block (4: the tiny vocabulary's rows 0.5 us more, 32 rows of 126464 0.4 less)
   const uint32_t want = __builtin_amdgcn_readfirstlane(sh.value), even = want | want << 16;
   const uint32_t care = want == 0 ? 0x7fffu : 0xffffu;
   const bool back = sh.rank > sh.count / 2;
   const uint32_t left = back ? sh.count - 1 - sh.rank : sh.rank;
   const int shift = (int)((uintptr_t)x & 15) / 2;  // chunk c holds ids 8 c - shift ..
   const u32x4_t* xv = reinterpret_cast<const u32x4_t*>(x - shift);
-  const int nch = (V + shift + 7) >> 3, blocks = (nch + 4 * NT - 1) / (4 * NT);
+  const int nch = (V + shift + 7) >> 3, blocks = (nch + CH * NT - 1) / (CH * NT);
   auto whole = [&](int c) { return c * 8 >= shift && c * 8 - shift + 8 <= V; };
-  auto first_chunk = [&](int i) { return (back ? blocks - 1 - i : i) * 4 * NT + tid; };
-  u32x4_t w[4];
+  auto first_chunk = [&](int i) { return (back ? blocks - 1 - i : i) * CH * NT + tid; };
+  u32x4_t w[CH];
+  auto load = [&](int i) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (whole(first_chunk(0) + k * NT)) w[k] = xv[first_chunk(0) + k * NT];
+    for (int k = 0; k < CH; ++k)
+      if (whole(first_chunk(i) + k * NT)) w[k] = xv[first_chunk(i) + k * NT];
+  };
+  load(0);
   uint32_t seen = 0;
   for (int i = 0; i < blocks; ++i) {
     const int c0 = first_chunk(i);
-    uint32_t hits[4];
+    uint32_t hits[CH];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < CH; ++k) {
       const int c = c0 + k * NT, id = c * 8 - shift;
       hits[k] = 0;
       if (whole(c)) {
@@ -657,26 +660,25 @@ __device__ __forceinline__ void find_id(Sh& sh, const uint16_t* x, int V, int ma
       }
       if ((uint32_t)(mask_id - id) < 8u) hits[k] &= ~(1u << (mask_id - id));
     }
-    if (i + 1 < blocks) {
+    // ahead where the id is likely to be further on: blocks read for nothing, always, took 235 us for 4096
+    // rows and not 228
+    const bool ahead = i + 1 < blocks && (uint64_t)(left - seen) * blocks > sh.count;
+    if (ahead) load(i + 1);
+    uint32_t own[CH], inc[CH];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (whole(first_chunk(i + 1) + k * NT)) w[k] = xv[first_chunk(i + 1) + k * NT];
-    }
-    uint32_t own[4], inc[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < CH; ++k) {
       own[k] = __popc(hits[k]);
       inc[k] = 0;
       if (__any(hits[k] != 0)) inc[k] = wave_scan(own[k]);
       if (lane == 63) sh.tot[i & 1][k * NW + wave] = inc[k];
     }
     __syncthreads();
-    static_assert(4 * NW <= 64, "a total of each wavefront and chunk to a lane");
-    const uint32_t all = wave_scan(lane < 4 * NW ? sh.tot[i & 1][lane] : 0u), total = lane_value(all, 63);
+    static_assert(CH * NW <= 64, "a total of each wavefront and chunk to a lane");
+    const uint32_t all = wave_scan(lane < CH * NW ? sh.tot[i & 1][lane] : 0u), total = lane_value(all, 63);
     if (left < seen + total) {
       const uint32_t at = back ? total - 1 - (left - seen) : left - seen;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < CH; ++k) {
         const int o = k * NW + wave;
         const uint32_t before = (o > 0 ? lane_value(all, o - 1) : 0) + inc[k] - own[k];
         if (before <= at && at < before + own[k]) {
@@ -688,6 +690,7 @@ __device__ __forceinline__ void find_id(Sh& sh, const uint16_t* x, int V, int ma
       break;
     }
     seen += total;
+    if (!ahead && i + 1 < blocks) load(i + 1);
   }
   __syncthreads();
 }
@@ -864,7 +867,7 @@ hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s) {
   // Up to a row per CU: 1024 threads, 32 x 126464 in 21.9 us against 25.0 with 512.  More: 512, three
   // rows to a CU, 4096 x 126464 in 253 us against 378 with 1024 and one, 303 with 1024 in 64 registers
   // and two, 310 with 512 in 64 registers and four (both spill); 777 x 50257 in 41.5 against 57, 54, 47
-  // (today's 229 and 39.3 us with the sums' entries side by side).
+  // (225 and 38 us since).
   const bool many = a.rows > 256;
   if (many) hipLaunchKernelGGL((k_vocab_sample<512, true>), dim3(a.rows), dim3(512), 0, s, a);
   else hipLaunchKernelGGL((k_vocab_sample<1024, false>), dim3(a.rows), dim3(1024), 0, s, a);
