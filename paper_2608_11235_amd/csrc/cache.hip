@@ -13,8 +13,7 @@
 
 #include <algorithm>
 
-#include "common.hpp"
-#include "internal.hpp"
+#include "cached.hpp"
 
 namespace cora {
 

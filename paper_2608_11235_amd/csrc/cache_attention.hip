@@ -21,8 +21,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "common.hpp"
-#include "internal.hpp"
+#include "cached.hpp"
 
 namespace cora {
 

@@ -105,26 +105,3 @@ __device__ __forceinline__ TopState merge(TopState x, TopState y) {
   r.arg = x.m > y.m ? x.arg : (y.m > x.m ? y.arg : min(x.arg, y.arg));
   return r;
 }
-
-// ---- wavefront sums by lane moves (DPP) -----------------------------------------------------
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t v) {  // 0 where a lane has no source
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double moved(double v) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = moved<CTRL, ROWS>((uint32_t)b), hi = moved<CTRL, ROWS>((uint32_t)(b >> 32));
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// inclusive sums over the lanes: inside rows of 16, then the rows before
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {
-  v += moved<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
-  v += moved<0x112, 0xf>(v);
-  v += moved<0x114, 0xf>(v);
-  v += moved<0x118, 0xf>(v);
-  v += moved<0x142, 0xa>(v);  // row_bcast 15, 31
-  v += moved<0x143, 0xc>(v);
-  return v;
-}

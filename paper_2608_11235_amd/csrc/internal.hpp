@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "cora.h"
-
 namespace cora {
 
 // ---- weight init ------------------------------------------------------------------------
@@ -197,73 +195,5 @@ hipError_t launch_vocab_top1_split(const VocabGateArgs& a, const VocabSplit& sp,
 // decision rules per batch row, reading the scores of rows [row_begin, row_begin + n_rows)
 // (n_rows == out_ld) or of the active block (row_begin < 0)
 hipError_t launch_gate_rules(const VocabGateArgs& a, hipStream_t s);
-
-// ---- sampling -----------------------------------------------------------------------------
-// Row r of the logits starts at logits + r * ld.  top_k, top_p, min_p may be null (off).
-struct SampleArgs {
-  const uint16_t* logits;
-  int rows, V;
-  int64_t ld;
-  int mask_id;  // -1: none
-  const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p; const float* u;
-  int32_t* token; float* conf;
-};
-hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s);
-
-// ---- paged K/V cache -----------------------------------------------------------------------
-// A page of one kv head holds K and V of its positions as 32-key groups of 1 KB blocks, each the
-// operand of one 16x16x32 MFMA in lane order (lane r + 16 g, 8 elements a lane).
-// K: two halves (key bit 2) of head_dim / 32 blocks of 16 keys x 32 dimensions.  Key 8 (r / 4) + 4 half
-// + r % 4 of the group is row r, so that the scores of a lane group are 8 neighbouring keys.
-__host__ __device__ inline int cache_k_index(int p, int d, int hd) {
-  const int k = p & 31;
-  return (p >> 5) * 32 * hd + ((k >> 2) & 1) * 16 * hd + (d >> 5) * 512 + ((d >> 3) & 3) * 128 +
-         (4 * (k >> 3) + (k & 3)) * 8 + (d & 7);
-}
-// V: head_dim / 16 blocks of 16 dimensions x 32 keys.
-__host__ __device__ inline int cache_v_index(int p, int d, int hd) {
-  return (p >> 5) * 32 * hd + (d >> 4) * 512 + ((p >> 3) & 3) * 128 + (d & 15) * 8 + (p & 7);
-}
-constexpr int CACHE_MAX_BATCH = CORA_CACHE_MAX_BATCH;
-struct CachePlanArgs {
-  int32_t *table, *len, *free, *n_free;
-  const int32_t *start, *count;
-  int32_t *cu, *positions, *slots, *status;
-  int B, max_pages, n_pages, shift, rows, reset;  // page size 1 << shift
-  int rows_apart;                                 // set by the launcher
-};
-hipError_t launch_cache_plan(CachePlanArgs a, hipStream_t s);
-// Rows [0, cu_end[0]) of x = [q | k | v], bf16 (xb) or the sum of `splits` fp32 slabs and the bias
-// (xf), row stride ld.  q may be null.
-struct CacheStoreArgs {
-  const uint16_t* xb; const float* xf; int64_t ld, slab; int splits; const float* bias;
-  int rows, H, Hkv, shift, n_slots;
-  const int32_t *positions, *slots, *cu_end;
-  const float* rope; int n_pos;  // (cos, sin) [n_pos][hd / 2], null: no rotation
-  uint16_t *k, *v, *q;
-};
-// paired: a head's dimensions come pair-interleaved (ROW_ROPE_PAIR) and stay so
-hipError_t launch_cache_store(const CacheStoreArgs& a, int hd, bool paired, hipStream_t s);
-struct CacheAttnArgs {
-  const uint16_t *q, *k, *v;
-  uint16_t* out;
-  const int32_t *table, *len, *start, *cu;
-  float *part_o, *part_ml;  // [rows][H][splits][hd], [rows][H][splits][2]
-  int B, rows, H, Hkv, shift, n_pages, max_pages, causal, panels;
-  float scale_log2;
-  int G, tiles, per_request, splits, chunk;  // set from the plan
-};
-// tile_rows (token, head) rows a workgroup, `splits` ranges of `chunk` keys (the last takes the
-// rest).  Made from sizes a caller keeps from call to call, never from the lengths on the device,
-// so that a row's sums do not depend on what else is in the batch.
-struct CacheAttnPlan {
-  int tile_rows, tiles, splits, chunk;
-  int per_request;  // tiles of each request where they have about as many rows, or 0
-  int workgroups;   // of the few-rows kernel
-  size_t ws_floats;
-};
-CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int max_count, int max_len,
-                                   int num_cus, size_t most_ws_floats);
-hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnPlan& p, int hd, float* ws, hipStream_t s);
 
 }  // namespace cora

@@ -14,6 +14,7 @@
 #include <stdexcept>
 
 #include "common.hpp"
+#include "cached.hpp"
 #include "internal.hpp"
 
 using namespace cora;
