@@ -348,8 +348,8 @@ cora_status cora_cache_store(const cora_cache *cache, int32_t layer, const void 
 
 /* Attention of the chunk's rows over their requests' pages: query head h reads kv head
  * h / (n_heads / n_kv_heads); keys j < len, and with causal != 0 j <= the row's position.
- * d_q, d_out bf16 [rows, n_heads, head_dim].  A row without a key is zero; rows from cu[B] on
- * are left alone; what the pages hold behind len is never used.  Read: chunk start, cu; pages
+ * d_q, d_out bf16 [rows, n_heads, head_dim].  A row without a key is zero; rows before cu[0]
+ * and from cu[B] on are left alone; what the pages hold behind len is never used.  Read: chunk start, cu; pages
  * table, len.  max_count and max_len are the most rows of a request and the longest len to
  * expect (<= 0: rows and max_pages * page_size); they choose tiles and key ranges, and with
  * them the order of the sums, and longer requests are still computed in full.  workspace of

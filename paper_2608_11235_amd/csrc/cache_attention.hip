@@ -69,10 +69,10 @@ struct Work {
 // first, and the first range, which holds the short ones whole, fills the gaps at the end.  With
 // `per_request` tiles a request (every request has about as many rows) a workgroup's place follows from
 // its number, the kv head the fastest and the later tiles, which see more keys under the causal mask,
-// before the earlier ones (382 us against 402).  Else (a prompt beside single tokens) tile t belongs to the request
-// b with base_b <= t < base_(b+1), base_b = cu_b G / RT + b, which leaves each request at least as many
-// tiles as it fills and needs no pass over the lengths, and an XCD takes a range of kv heads and tiles,
-// whose keys its L2 then holds.
+// before the earlier ones (382 us against 402).  Else (a prompt beside single tokens) tile t belongs to
+// the request b with base_b <= t < base_(b+1), base_b = cu_b G / RT + b, which leaves each request at
+// least as many tiles as it fills and needs no pass over the lengths, and an XCD takes a range of kv
+// heads and tiles, whose keys its L2 then holds.
 template <int RT>
 __device__ __forceinline__ bool first_tile(const CacheAttnArgs& a, Work& w) {
   int li = blockIdx.x;
@@ -94,7 +94,7 @@ __device__ __forceinline__ bool first_tile(const CacheAttnArgs& a, Work& w) {
   }
   w.cu = uniform(clamped_cu(a, w.b));
   w.n_rows = (uniform(clamped_cu(a, w.b + 1)) - w.cu) * a.G;
-  if (w.row0 >= w.n_rows) return false;
+  if (w.row0 < 0 || w.row0 >= w.n_rows) return false;  // below 0: a cu that starts late or does not ascend
   w.start = uniform(a.start[w.b]);
   w.len = uniform(clamped_len(a, w.b));
   const int n = pieces(a, w.len);
@@ -666,6 +666,7 @@ __global__ __launch_bounds__(256) void k_cache_attend_merge(CacheAttnArgs a) {
   const int token = (int)(i / (uint32_t)a.H), head = (int)(i % (uint32_t)a.H);
   if (token >= clamped_cu(a, a.B)) return;
   const int b = owner_by_lanes(a.B, token, [&](int x) { return clamped_cu(a, x); });
+  if (token < clamped_cu(a, b) || token >= clamped_cu(a, b + 1)) return;  // no request's
   const int len = clamped_len(a, b);
   const int used = pieces(a, len);
   if (used == 1) return;  // written already

@@ -62,6 +62,26 @@ def test_attention_requests_without_rows():
         assert (out == 9).all()
 
 
+@pytest.mark.parametrize("max_count,max_len", [(1, 1), (1, 9000), (30, 9000), (30, 300), (0, 0)])
+def test_attention_rows_before_the_first_request(max_count, max_len):
+    """cu need not start at 0: rows of no request stay as they are."""
+    require_gpu()
+    rng = np.random.default_rng(2)
+    lens, count = [900, 2100, 64, 7], [40, 3, 64, 1]
+    cache, chunk, q, ks, vs, T = requests(rng, lens, count, 64, 8, 2, 32, rows=sum(count) + 20)
+    want = torch.full_like(q, 9.0)
+    cache_attention(cache, 0, q, chunk, causal=True, out=want, max_count=max_count, max_len=max_len)
+    for late in (1, 5, 20):
+        shifted = torch.zeros_like(q)
+        shifted[late:late + T] = q[:T]
+        chunk.cu.add_(late)
+        out = torch.full_like(q, 9.0)
+        cache_attention(cache, 0, shifted, chunk, causal=True, out=out, max_count=max_count, max_len=max_len)
+        chunk.cu.sub_(late)
+        assert (out[:late] == 9).all() and (out[late + T:] == 9).all()
+        assert torch.equal(out[late:late + T], want[:T])
+
+
 def test_attention_expected_lengths_that_grow():
     """A max_len of its own for every call: the sizes kept on the host stay few, results the same."""
     require_gpu()
