@@ -285,19 +285,22 @@ def _rows_2d(t, name, dtypes):
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a GPU tensor (got device {t.device})")
     n, width = t.shape
-    if (width > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < width):
+    ld, step = t.stride()
+    if (width > 1 and step != 1) or (n > 1 and ld < width):
         raise ValueError(f"{name}: strides {t.stride()}, expected rows of stride 1 that do not overlap")
-    return t.get_device(), t.stride(0) if n > 1 else width
+    return t.get_device(), ld if n > 1 else width
 
 
 def _call(device, func, *args, stream=None):
     """Call the library with `device` current, on the stream given or torch's current one there."""
     f = getattr(_lib.load(), func)
+    # the address alone: a torch.cuda.Stream made around it costs a microsecond a call
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == device:
-        status = f(*args, (stream or torch.cuda.current_stream(device)).cuda_stream)
+        status = f(*args, handle)
     else:
         with torch.cuda.device(device):
-            status = f(*args, (stream or torch.cuda.current_stream(device)).cuda_stream)
+            status = f(*args, handle)
     if status:
         check(status, func)
 
