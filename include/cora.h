@@ -314,7 +314,8 @@ typedef struct {
  * another.  start, count int32 [B] are the caller's; cora_cache_plan writes cu int32 [B + 1]
  * (request b's rows are [cu[b], cu[b+1])), status int32 [B] and, for `rows` rows, positions and
  * slots int32 [rows] (slot = page * page_size + position in the page; both -1 in rows from
- * cu[B] on).  `rows` is the capacity: fixed for a program, whatever the live count. */
+ * cu[B] on, the slot where the table holds no page of the pool).  `rows` is the capacity: fixed
+ * for a program, whatever the live count. */
 typedef struct {
   const int32_t *start, *count;
   int32_t *cu, *positions, *slots, *status;

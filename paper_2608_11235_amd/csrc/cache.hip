@@ -92,7 +92,8 @@ __device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_
   for (int u = 0; u < 4; ++u) {
     if (r[u] >= (uint32_t)a.rows) continue;
     a.positions[r[u]] = pos[u];
-    a.slots[r[u]] = pos[u] < 0 ? -1 : (page[u] << a.shift) + (pos[u] & ((1 << a.shift) - 1));
+    const bool known = pos[u] >= 0 && (uint32_t)page[u] < (uint32_t)a.n_pages;  // a table's nonsense stays outside
+    a.slots[r[u]] = known ? (page[u] << a.shift) + (pos[u] & ((1 << a.shift) - 1)) : -1;
   }
 }
 

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2608_11235_amd import cache_attention, cache_plan, cache_store, rope_table, Chunk
+from paper_2608_11235_amd import Chunk, KVCache, cache_attention, cache_plan, cache_store, rope_table
 from tests import cache_ref as ref
 from tests.gpu_common import log_case, require_gpu
 from tests.test_gpu_cache import compare, filled, put, requests
@@ -91,6 +91,24 @@ def test_attention_expected_lengths_that_grow():
     for n in range(2, 600):
         got = cache_attention(cache, 0, q, chunk, max_count=1, max_len=n)
     assert torch.equal(got, want) and len(cache._workspaces) <= 256
+
+
+@pytest.mark.parametrize("page", [1 << 27, (1 << 27) + 1, -(1 << 27), 4, -1])
+@pytest.mark.parametrize("rows", [8, 9000])
+def test_plan_pages_that_are_not_there(page, rows):
+    """A page number whose slots would wrap around to those of another request gives no slot."""
+    require_gpu()
+    cache, chunk = KVCache(1, 4, 1, 64, 32, 1, 3), Chunk(1, rows)
+    put(cache.table, [[page, 1, 2]]); put(cache.len, [40])
+    put(chunk.start, [30]); put(chunk.count, [4])
+    cache_plan(cache, chunk)
+    assert chunk.status.tolist() == [0] and chunk.positions[:5].tolist() == [30, 31, 32, 33, -1]
+    assert chunk.slots[:5].tolist() == [-1, -1, 32, 33, -1]
+    cache.k.zero_(); cache.v.zero_()
+    x = torch.ones((rows, 3 * 64), dtype=torch.bfloat16, device="cuda")
+    q = cache_store(cache, 0, x, 1, chunk)
+    used = ref.natural(cache.k[0], ref.offsets(32, 64)[0])
+    assert (q[:2] == 0).all() and (used[1, 0, :2] == 1).all() and int((used != 0).sum()) == 2 * 64
 
 
 @pytest.mark.parametrize("H,Hkv", [(9, 3), (13, 13)])
