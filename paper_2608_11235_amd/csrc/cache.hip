@@ -25,60 +25,69 @@ constexpr int PT = 1024;  // threads of the plan's workgroup
 // fits the pool and the chunk, which are smaller
 __device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
 
+// inclusive saturating sums over the lanes of each row of 16
+__device__ __forceinline__ uint32_t row_scan(uint32_t v) {
+  v = add_sat(v, moved<0x111, 0xf>(v));
+  v = add_sat(v, moved<0x112, 0xf>(v));
+  v = add_sat(v, moved<0x114, 0xf>(v));
+  return add_sat(v, moved<0x118, 0xf>(v));
+}
+
 // inclusive sums of two values over the workgroup, `carry` added and advanced by the totals
 __device__ __forceinline__ void block_scan(uint32_t (&v)[2], uint32_t (&carry)[2], uint32_t (*part)[PT / 64]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t u = __shfl_up(v[k], o, 64);
-      if (lane >= o) v[k] = add_sat(v[k], u);
-    }
-  if (lane == 63) part[0][wave] = v[0], part[1][wave] = v[1];
-  __syncthreads();
+  static_assert(PT / 64 == 16, "a row of lanes holds the wavefronts' totals");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    uint32_t before = carry[k];
+    v[k] = row_scan(v[k]);
+    v[k] = add_sat(v[k], moved<0x142, 0xa>(v[k]));  // row_bcast 15, 31
+    v[k] = add_sat(v[k], moved<0x143, 0xc>(v[k]));
+    if (lane == 63) part[k][wave] = v[k];
+  }
+  __syncthreads();
+  const int totals = (int)row_scan(lane < 32 ? part[lane >> 4][lane & 15] : 0u);
 #pragma unroll
-    for (int w = 0; w < PT / 64; ++w) {
-      const uint32_t p = part[k][w];
-      if (w < wave) before = add_sat(before, p);
-      carry[k] = add_sat(carry[k], p);
-    }
-    v[k] = add_sat(v[k], before);
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t before = wave > 0 ? (uint32_t)__builtin_amdgcn_readlane(totals, 16 * k + wave - 1) : 0u;
+    v[k] = add_sat(add_sat(v[k], before), carry[k]);
+    carry[k] = add_sat(carry[k], (uint32_t)__builtin_amdgcn_readlane(totals, 16 * k + 15));
   }
   __syncthreads();
 }
 
-// b[u]: the greatest in [0, B) with first[b] <= i[u]  (first[0] = 0, ascending); four at once
-__device__ __forceinline__ void owners(const uint32_t* first, int B, const uint32_t (&i)[4], int (&b)[4]) {
-  b[0] = b[1] = b[2] = b[3] = 0;
+// the greatest b in [0, B) with first[b] <= i  (first[0] = 0, ascending)
+__device__ __forceinline__ int owner(const uint32_t* first, int B, uint32_t i) {
+  int b = 0;
   for (int step = 1 << (31 - __clz(B)); step > 0; step >>= 1)
+    if (b + step < B && first[b + step] <= i) b += step;
+  return b;
+}
+// of i and the three after it, which mostly have the same; first[B] is the end
+__device__ __forceinline__ void owners(const uint32_t* first, int B, uint32_t i, int (&b)[4]) {
+  b[0] = owner(first, B, i);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int n = b[u] + step;
-      if (n < B && first[n] <= i[u]) b[u] = n;
-    }
+  for (int u = 1; u < 4; ++u) {
+    b[u] = b[u - 1];
+    if (first[b[u] + 1] > i + u || i + u >= first[B]) continue;
+    ++b[u];  // the next one, unless that is empty
+    if (first[b[u] + 1] <= i + u) b[u] = owner(first, B, i + u);
+  }
 }
 
 __device__ __forceinline__ int pages_of(int len, int shift) { return (int)(((int64_t)len + (1 << shift) - 1) >> shift); }
 
-// Positions and slots of rows r0 + threadIdx + NT u, u < 4.  `top` != null: the pages that the call
-// takes are read from where they come from, since the table may not hold them yet.
-template <int NT>
-__device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_t* first_row, int total, int r0,
+// Positions and slots of rows r .. r + 3.  `top` != null: the pages that the call takes are read from
+// where they come from, since the table may not hold them yet.
+__device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_t* first_row, uint32_t r,
                                            const uint32_t* first_page, const uint32_t* have, const int32_t* top) {
-  uint32_t r[4];
-  int b[4], pos[4], page[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) r[u] = r0 + threadIdx.x + NT * u;
-  owners(first_row, a.B, r, b);
+  const uint32_t total = first_row[a.B];
+  int b[4] = {}, pos[4], page[4];
+  if (r < total) owners(first_row, a.B, r, b);
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     page[u] = pos[u] = -1;
-    if (r[u] < (uint32_t)total) {
-      pos[u] = a.start[b[u]] + (int)(r[u] - first_row[b[u]]);
+    if (r + u < total) {
+      pos[u] = a.start[b[u]] + (int)(r + u - first_row[b[u]]);
       const int j = pos[u] >> a.shift;
       if (first_page && j >= (int)have[b[u]]) {
         const int i = (int)first_page[b[u]] + j - (int)have[b[u]];
@@ -90,10 +99,10 @@ __device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_
   }
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    if (r[u] >= (uint32_t)a.rows) continue;
-    a.positions[r[u]] = pos[u];
+    if (r + u >= (uint32_t)a.rows) continue;
+    a.positions[r + u] = pos[u];
     const bool known = pos[u] >= 0 && (uint32_t)page[u] < (uint32_t)a.n_pages;  // a table's nonsense stays outside
-    a.slots[r[u]] = known ? (page[u] << a.shift) + (pos[u] & ((1 << a.shift) - 1)) : -1;
+    a.slots[r + u] = known ? (page[u] << a.shift) + (pos[u] & ((1 << a.shift) - 1)) : -1;
   }
 }
 
@@ -101,7 +110,9 @@ __device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_
 
 // Bound by latency: a chain of loads, scans and stores of one workgroup.  Requests' sums are made once
 // where none is refused, and after a reset, which leaves page i at the stack's i'th place, no page is
-// read back.  64 requests of one token 6.0 us; 512 prompts of 545 thousand rows 13.0 us and 7.1 for the rows.
+// read back.  64 requests of one token 4.8 us (a search of
+// its own for every page and row, scans by lane exchanges through LDS: 6.0); 512 prompts of 545
+// thousand rows 7.9 us (13.0) and 5.9 for the rows (7.2).
 __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
   extern __shared__ uint32_t lds[];
   const int tid = threadIdx.x, B = a.B;
@@ -112,12 +123,14 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
   const int most = a.max_pages << a.shift;
   int n_free = a.reset ? a.n_pages : min(max(a.n_free[0], 0), a.n_pages);
   auto length = [&](int b) { return a.reset ? 0 : min(max(a.len[b], 0), most); };
+  // the first requests' numbers, one a thread, are read once
+  const int own_count = tid < B ? a.count[tid] : 0, own_start = tid < B ? a.start[tid] : 0, own_len = tid < B ? length(tid) : 0;
 
   // what each request asks for, and whether it gets it; pages that finished requests give back first
   uint32_t sum[2] = {0, 0};  // pages, rows
   uint32_t back[2] = {0, 0};
-  bool returns = false, refused = false;
-  for (int b = tid; b < B; b += PT) returns |= a.count[b] < 0;
+  bool returns = own_count < 0, refused = false;
+  for (int b = tid + PT; b < B; b += PT) returns |= a.count[b] < 0;
   if (a.reset) {
     for (int i = tid; i < a.n_pages; i += PT) a.free[i] = a.n_pages - 1 - i;
   } else if (__syncthreads_or(returns)) {
@@ -128,19 +141,15 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
       block_scan(v, back, part);
       if (b < B) first_page[b] = v[0] - n;
     }
+    if (tid == 0) first_page[B] = back[0];
     __syncthreads();  // first_page is whole
     const uint32_t given = min(back[0], (uint32_t)(a.n_pages - n_free));  // more only if a table holds a page twice
-    for (uint32_t i0 = 0; i0 < given; i0 += 4 * PT) {
-      uint32_t i[4];
+    for (uint32_t i = 4 * tid; i < given; i += 4 * PT) {
       int b[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) i[u] = i0 + tid + PT * u;
       owners(first_page, B, i, b);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (i[u] < given)
-          a.free[n_free + i[u]] = a.table[(int64_t)b[u] * a.max_pages + (i[u] - first_page[b[u]])];
-      }
+      for (int u = 0; u < 4; ++u)
+        if (i + u < given) a.free[n_free + i + u] = a.table[(int64_t)b[u] * a.max_pages + (i + u - first_page[b[u]])];
     }
     n_free += (int)given;
     __syncthreads();  // first_page is used anew, and the pages below are taken from the stack
@@ -151,7 +160,7 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
     int status = 0;
     uint32_t need = 0, count = 0, held = 0;
     if (b < B) {
-      const int start = a.start[b], len = length(b), n = max(a.count[b], 0);
+      const int start = b0 ? a.start[b] : own_start, len = b0 ? length(b) : own_len, n = max(b0 ? a.count[b] : own_count, 0);
       held = (uint32_t)pages_of(len, a.shift);
       if (n > 0) {
         if (start < 0 || start > len || (int64_t)start + n > most) status = CORA_ERR_INVALID_ARG;
@@ -193,31 +202,33 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
   }
   const uint32_t pages = sum[0], rows = sum[1];
   if (tid == 0) {
+    first_page[B] = pages;
     first_row[B] = rows;
     a.n_free[0] = n_free - (int)pages;
   }
   __syncthreads();
 
   const int32_t* top = a.reset ? nullptr : a.free + n_free - 1;
-  for (uint32_t i0 = 0; i0 < pages; i0 += 4 * PT) {
-    uint32_t i[4];
+  // the pages from the last thread on, the rows from the first, so that few of both go side by side
+  for (uint32_t i = 4 * (PT - 1 - tid); i < pages; i += 4 * PT) {
     int b[4], page[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) i[u] = min(i0 + tid + PT * u, pages - 1);
     owners(first_page, B, i, b);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) page[u] = top ? top[-(int)i[u]] : (int)i[u];
+    for (int u = 0; u < 4; ++u)
+      if (i + u < pages) page[u] = top ? top[-(int)(i + u)] : (int)(i + u);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)  // those past the last one write it once more
-      a.table[(int64_t)b[u] * a.max_pages + have[b[u]] + (i[u] - first_page[b[u]])] = page[u];
+    for (int u = 0; u < 4; ++u)
+      if (i + u < pages) a.table[(int64_t)b[u] * a.max_pages + have[b[u]] + (i + u - first_page[b[u]])] = page[u];
   }
   if (!a.rows_apart)
-    for (int r0 = 0; r0 < a.rows; r0 += 4 * PT) place_rows<PT>(a, first_row, (int)rows, r0, first_page, have, top);
+    for (uint32_t r = 4 * tid; r < (uint32_t)a.rows; r += 4 * PT) place_rows(a, first_row, r, first_page, have, top);
   for (int b = tid; b <= B; b += PT) {
     a.cu[b] = (int)first_row[b];
     if (b == B) continue;
     const int n = (int)(first_row[b + 1] - first_row[b]);
-    a.len[b] = a.count[b] < 0 ? 0 : (n > 0 ? max(length(b), a.start[b] + n) : length(b));
+    const bool own = b == tid;
+    const int count = own ? own_count : a.count[b], start = own ? own_start : a.start[b], len = own ? own_len : length(b);
+    a.len[b] = count < 0 ? 0 : (n > 0 ? max(len, start + n) : len);
   }
 }
 
@@ -226,7 +237,7 @@ __global__ __launch_bounds__(256) void k_cache_rows(CachePlanArgs a) {
   extern __shared__ uint32_t lds[];
   for (int b = threadIdx.x; b <= a.B; b += 256) lds[b] = (uint32_t)a.cu[b];
   __syncthreads();
-  place_rows<256>(a, lds, (int)lds[a.B], blockIdx.x * 1024, nullptr, nullptr, nullptr);
+  place_rows(a, lds, (blockIdx.x * 256 + threadIdx.x) * 4, nullptr, nullptr, nullptr);
 }
 
 hipError_t launch_cache_plan(CachePlanArgs a, hipStream_t s) {
