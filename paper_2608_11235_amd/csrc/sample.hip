@@ -833,6 +833,8 @@ __global__ __launch_bounds__(NT, NT == 512 ? 6 : 4) void k_vocab_sample(SampleAr
     count_entries<Bins, NT>(sh, 0);
     __syncthreads();
     first = least_first<NT>(sh);
+    // a multiple of 65536 equal negative logits and no other leave no count at all
+    if (PAIRED && first == INT_MAX && sh.uncounted != (uint32_t)a.V) special = OTHER;
   }
   // Numbers of -2^19 and below beside a maximum of at least -2^18 weigh exp(-2^18 / T), which is
   // 0 in 64 bits for T up to 350, and can then be left out.
