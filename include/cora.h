@@ -371,9 +371,9 @@ cora_status cora_cache_attention(const cora_cache *cache, int32_t layer, const c
  * attending to the request's pages (both directions, or causal), LM head on every row: bf16
  * logits [rows, V].  The cache has the model's layers, kv heads and head_dim; its K holds the
  * head's dimensions pair-interleaved (j at 2j, j + hd/2 at 2j + 1).  Rows from cu[B] on compute on
- * whatever d_tokens holds there, their logits are unspecified.  Positions stay below max_seq
- * (a row beyond it is not stored).  Kernel choices follow chunk->rows, B, max_count and max_len,
- * not the live rows.  CORA_ERR_UNSUPPORTED when rows * (n_heads + 2 n_kv_heads) * head_dim
+ * whatever d_tokens holds there, their logits are unspecified.  max_seq bounds the rows of a
+ * pass, not their positions, which go as far as the table's.  Kernel choices follow chunk->rows, B,
+ * max_count and max_len, not the live rows.  CORA_ERR_UNSUPPORTED when rows * (n_heads + 2 n_kv_heads) * head_dim
  * exceeds the model's fp32 workspace (2^25 elements on this GPU) or rows exceed max_batch *
  * max_seq: run a longer prompt in several chunks.  Uses the model's workspace.  Asynchronous. */
 cora_status cora_forward_cached(cora_model *model, const cora_cache *cache, const cora_pages *pages,

@@ -306,7 +306,7 @@ __device__ __forceinline__ u32x4_t pack8(const float (&v)[8]) {
 __device__ __forceinline__ bool slot_of(const CacheStoreArgs& a, int r, int& slot) {
   slot = a.slots[r];
   const int pos = a.positions[r];
-  return slot >= 0 && slot < a.n_slots && pos >= 0 && (!a.rope || pos < a.n_pos);
+  return slot >= 0 && slot < a.n_slots && pos >= 0 && (!a.rope || a.rope_by_row || pos < a.n_pos);
 }
 
 // q and k of 32 rows and NH x HPW heads from h0 on: hd / 16 threads per row and head, 16 dimensions
@@ -333,7 +333,8 @@ __device__ __forceinline__ void store_qk(const CacheStoreArgs& a, int r, int h0)
       for (int e = 0; e < 8; ++e) x0[n][e] = x1[n][e] = 0.f;
   } else if (a.rope) {
     // (cos, sin) of the 8 pairs: pair p of the head turns by pos theta^(-2 p / HD)
-    const f32x4_t* cs = reinterpret_cast<const f32x4_t*>(a.rope + ((int64_t)a.positions[r] * (HD / 2) + j * 8) * 2);
+    const int at = a.rope_by_row ? r : a.positions[r];
+    const f32x4_t* cs = reinterpret_cast<const f32x4_t*>(a.rope + ((int64_t)at * (HD / 2) + j * 8) * 2);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       const f32x4_t c = cs[p];
@@ -460,6 +461,36 @@ __global__ __launch_bounds__(256) void k_cache_store(CacheStoreArgs a) {
     const int r = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 8;
     if (r < rows) store_v<HD, F32>(a, rows, r, (group - qk) * HPW);
   }
+}
+
+// The angles of a chunk's rows in a pass whose cache goes beyond the table of angles: once a pass, one
+// thread a pair, in 64 bits (an angle of 2^30 in 32 bits is off by whole turns).
+__global__ __launch_bounds__(256) void k_rope_rows(const int32_t* positions, const int32_t* cu_end, const float* table,
+                                                   int n_pos, const double* freq, int rows, int half, float* out) {
+  const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+  const int r = (int)(i / half), j = (int)(i % half);
+  if (r >= min(rows, cu_end[0])) return;
+  const int pos = positions[r];
+  if (pos < 0) return;
+  f32x2_t cs;
+  if (pos < n_pos) {
+    cs = *reinterpret_cast<const f32x2_t*>(table + ((int64_t)pos * half + j) * 2);
+  } else {
+    double sn, c;
+    sincos(pos * freq[j], &sn, &c);
+    cs = f32x2_t{(float)c, (float)sn};
+  }
+  *reinterpret_cast<f32x2_t*>(out + i * 2) = cs;
+}
+
+hipError_t launch_rope_rows(const int32_t* positions, const int32_t* cu_end, const float* table, int n_pos,
+                            const double* freq, int rows, int half, float* out, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  const int64_t wgs = ((int64_t)rows * half + 255) / 256;
+  if (wgs > 0xffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_rope_rows, dim3((unsigned)wgs), dim3(256), 0, s, positions, cu_end, table, n_pos, freq, rows,
+                     half, out);
+  return hipGetLastError();
 }
 
 // Windows x heads of 128 from which a thread takes four: 43.3 against 46.6 us at 8192 and 20.4 against

@@ -49,8 +49,13 @@ struct CacheStoreArgs {
   int rows, H, Hkv, shift, n_slots;
   const int32_t *positions, *slots, *cu_end;
   const float* rope; int n_pos;  // (cos, sin) [n_pos][hd / 2], null: no rotation
+  int rope_by_row;               // `rope` holds the rows' own angles, [rows][hd / 2]
   uint16_t *k, *v, *q;
 };
+// out [rows][half]: (cos, sin) of the rows' positions times freq [half], from the table of n_pos
+// positions where that has them.  Rows from cu_end[0] on and those without a position are left alone.
+hipError_t launch_rope_rows(const int32_t* positions, const int32_t* cu_end, const float* table, int n_pos,
+                            const double* freq, int rows, int half, float* out, hipStream_t s);
 // paired: a head's dimensions come pair-interleaved (ROW_ROPE_PAIR) and stay so
 hipError_t launch_cache_store(const CacheStoreArgs& a, int hd, bool paired, hipStream_t s);
 struct CacheAttnArgs {

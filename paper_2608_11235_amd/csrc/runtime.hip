@@ -97,7 +97,9 @@ struct cora_model {
   float* h = nullptr;
   uint16_t *a = nullptr, *q = nullptr, *k = nullptr, *vt = nullptr;
   uint16_t *attn = nullptr, *u = nullptr, *logits = nullptr;
-  float* rope_cs = nullptr;  // (cos, sin) pairs
+  float* rope_cs = nullptr;     // (cos, sin) pairs [max_seq_pad][head_dim / 2]
+  double* rope_freq = nullptr;  // an angle a position, of each pair
+  float* rope_rows = nullptr;   // the pairs of a cached pass's rows, some beyond rope_cs
   int num_cus = 256;
   float* splitk_ws = nullptr;
   size_t splitk_ws_floats = 0;
@@ -240,7 +242,7 @@ extern "C" cora_status cora_model_create(const cora_model_cfg* cfg, uint64_t see
   size_t wsb = 3 * align_up(lmh_parts * 4) + align_up(lm_head_rows_held(V, d) * d * 2) + align_up(skw * 4) + align_up(M * d * 4) + align_up(M * (size_t)(d > m->hq ? d : m->hq) * 2) +
                align_up(Ms * m->hq * 2) + 2 * align_up(Ms * m->hkv * 2) +
                align_up(M * m->hq * 2) + align_up(M * m->f_pad * 2) + align_up(rows * V * 2) +
-               align_up((size_t)m->max_seq_pad * hd * 4) +
+               align_up((size_t)m->max_seq_pad * hd * 4) + align_up((size_t)hd / 2 * 8) + align_up(M * hd * 4) +
                // decode state
                align_up(BL * 4) * 3 + align_up(BL) + align_up(max_batch * 4) * 3 +
                align_up(BL * 4) * 2 + align_up(rows) + align_up((size_t)max_batch * max_seq * 4) +
@@ -288,6 +290,8 @@ extern "C" cora_status cora_model_create(const cora_model_cfg* cfg, uint64_t see
   m->u = a.take<uint16_t>(M * m->f_pad);
   m->logits = a.take<uint16_t>(rows * V);
   m->rope_cs = a.take<float>((size_t)m->max_seq_pad * hd);
+  m->rope_freq = a.take<double>(hd / 2);
+  m->rope_rows = a.take<float>(M * hd);
   m->s_tokens = a.take<int32_t>(BL);
   m->s_prev = a.take<int32_t>(BL);
   m->s_persist = a.take<int32_t>(BL);
@@ -346,13 +350,16 @@ extern "C" cora_status cora_model_create(const cora_model_cfg* cfg, uint64_t see
     // RoPE tables in fp64, stored fp32: angle = pos * theta^(-2j/hd)
     const int half = hd / 2;
     std::vector<float> cs((size_t)m->max_seq_pad * hd);
+    std::vector<double> freq(half);
+    for (int j = 0; j < half; ++j) freq[j] = pow((double)cfg->rope_theta, -2.0 * j / hd);
     for (int p = 0; p < m->max_seq_pad; ++p)
       for (int j = 0; j < half; ++j) {
-        const double ang = (double)p * pow((double)cfg->rope_theta, -2.0 * j / hd);
+        const double ang = (double)p * freq[j];
         cs[(size_t)p * hd + 2 * j] = (float)cos(ang);
         cs[(size_t)p * hd + 2 * j + 1] = (float)sin(ang);
       }
     HIP_TRY(hipMemcpyAsync(m->rope_cs, cs.data(), cs.size() * 4, hipMemcpyHostToDevice, s));
+    HIP_TRY(hipMemcpyAsync(m->rope_freq, freq.data(), freq.size() * 8, hipMemcpyHostToDevice, s));
     HIP_TRY(hipStreamSynchronize(s));
     return CORA_OK;
   }();
@@ -1169,6 +1176,11 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
       expected(max_len, (int64_t)p->max_pages * p->page_size), m->num_cus, m->splitk_ws_floats);
   GemmPlan gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 0, 0.0);
   if ((size_t)gp.splits * M * m->qkv_n > m->splitk_ws_floats) gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 1, 0.0);
+  // positions that the cache has room for and the model's table of angles does not
+  const bool beyond = (int64_t)p->max_pages * p->page_size > m->max_seq_pad;
+  if (beyond)
+    HIP_TRY(launch_rope_rows(ch->positions, ch->cu + p->B, m->rope_cs, m->max_seq_pad, m->rope_freq, M, hd / 2,
+                             m->rope_rows, s));
   HIP_TRY(launch_embed(d_tokens, m->embed, m->h, M, d, c.vocab, m->ones, c.n_layers ? m->a : nullptr, c.rms_eps, s));
   for (size_t l = 0; l < m->layers.size(); ++l) {
     GemmArgs g{m->a, m->layers[l].wqkv, W_BLOCKS, M, m->qkv_n, d, m->splitk_ws, m->qkv_n, nullptr, 1.0f};
@@ -1179,7 +1191,7 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
     st.rows = M; st.H = c.n_heads; st.Hkv = c.n_kv_heads; st.shift = page_shift(cache->page_size);
     st.n_slots = cache->n_pages * cache->page_size;
     st.positions = ch->positions; st.slots = ch->slots; st.cu_end = ch->cu + p->B;
-    st.rope = m->rope_cs; st.n_pos = m->max_seq;
+    st.rope = beyond ? m->rope_rows : m->rope_cs; st.n_pos = m->max_seq_pad; st.rope_by_row = beyond;
     st.k = cache->k + l * layer_elems; st.v = cache->v + l * layer_elems; st.q = m->q;
     HIP_TRY(launch_cache_store(st, hd, true, s));
     CacheAttnArgs a{};
