@@ -1064,6 +1064,7 @@ extern "C" cora_status cora_cache_store(const cora_cache* cache, int32_t layer, 
   if (cora_status e = check_cache(cache, layer)) return e;
   if (cora_status e = check_chunk(c)) return e;
   if (cora_status e = check_heads(n_heads, cache->n_kv_heads, c->rows)) return e;
+  if (c->rows == 0) return CORA_OK;  // no row: the arrays may be null
   if (!d_x || B < 1 || (d_rope && n_pos < 1)) return fail(CORA_ERR_INVALID_ARG, "null x, B < 1 or n_pos < 1");
   const int hd = cache->head_dim;
   if (ld < ((int64_t)n_heads + 2 * cache->n_kv_heads) * hd || ld % (x_f32 ? 4 : 8) != 0)
@@ -1126,6 +1127,7 @@ extern "C" cora_status cora_cache_attention(const cora_cache* cache, int32_t lay
   if (cora_status e = check_heads(n_heads, cache->n_kv_heads, c->rows)) return e;
   if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
     return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
+  if (c->rows == 0) return CORA_OK;  // no row: the arrays may be null
   if (!d_q || !d_out || !aligned16(d_q) || !aligned16(d_out))
     return fail(CORA_ERR_INVALID_ARG, "q and out must be given, aligned to 16 bytes");
   if (!(scale > 0.f) || !isfinite(scale)) return fail(CORA_ERR_INVALID_ARG, "scale must be positive and finite");
@@ -1156,7 +1158,7 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
                                            const cora_chunk* ch, const int32_t* d_tokens, int32_t max_count,
                                            int32_t max_len, int32_t causal, uint16_t* d_logits,
                                            void* hip_stream) try {
-  if (!m || !d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null argument");
+  if (!m) return fail(CORA_ERR_INVALID_ARG, "null model");
   if (cora_status e = check_cache(cache, 0)) return e;
   if (cora_status e = check_pages(p)) return e;
   if (cora_status e = check_chunk(ch)) return e;
@@ -1166,7 +1168,8 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
   if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
     return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
   const int M = ch->rows, d = c.d_model, hd = c.head_dim;
-  if (M == 0) return CORA_OK;
+  if (M == 0) return CORA_OK;  // no row: the arrays may be null
+  if (!d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null tokens or logits");
   if ((int64_t)M > (int64_t)m->max_batch * m->max_seq || (size_t)M * m->qkv_n > m->splitk_ws_floats)
     return fail(CORA_ERR_UNSUPPORTED, "chunk rows exceed the model's workspace: use several chunks");
   const hipStream_t s = S(hip_stream);
