@@ -294,8 +294,13 @@ def _rows_2d(t, name, dtypes):
 def _call(device, func, *args, stream=None):
     """Call the library with `device` current, on the stream given or torch's current one there."""
     f = getattr(_lib.load(), func)
-    # the address alone: a torch.cuda.Stream made around it costs a microsecond a call
-    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if stream is None:
+        # the address alone: a torch.cuda.Stream made around it costs a microsecond a call
+        handle = torch._C._cuda_getCurrentRawStream(device)
+    else:
+        if stream.device_index != device:
+            raise ValueError(f"stream: on cuda:{stream.device_index}, the tensors are on cuda:{device}")
+        handle = stream.cuda_stream
     if torch.cuda.current_device() == device:
         status = f(*args, handle)
     else:
