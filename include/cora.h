@@ -269,7 +269,8 @@ typedef struct {
  * greedy row gives cora_vocab_gate's top1 and conf.  A row without an allowed id gives token
  * -1 and confidence 0; a NaN at an allowed id makes the row's confidence NaN.  Rows that hold
  * +inf, NaN, or finite logits of magnitude >= 2^19 or in (0, 2^-44) that can matter take
- * several passes.  Allocates nothing, needs no workspace.  Asynchronous. */
+ * several passes.  R stays below 2^23, V does not exceed 2^30.  Allocates nothing, needs no
+ * workspace.  Asynchronous. */
 cora_status cora_vocab_sample(const uint16_t *d_logits, int32_t R, int32_t V, int64_t ld,
                               int32_t mask_id, const cora_sample_rows *rows, int32_t *d_token,
                               float *d_conf, void *hip_stream);
@@ -342,7 +343,9 @@ cora_status cora_cache_plan(cora_pages *pages, cora_chunk *chunk, int32_t reset,
  * d_q bf16 [rows, n_heads, head_dim] receives the rotated q (NULL: not wanted).  Of the chunk,
  * positions, slots and cu[B] are read.  Rows from cu[B] on are left alone; a row whose slot or
  * position lies outside the cache or the table is not stored and its q is zero.  The slots of a
- * chunk's rows must differ.  d_x, d_q, d_rope 16-byte aligned, rows too.  Asynchronous. */
+ * chunk's rows must differ.  d_x, d_q, d_rope 16-byte aligned, rows too.  CORA_ERR_UNSUPPORTED where
+ * rows and heads exceed one launch (2^24 workgroups of 32 rows and a head of 128 or two of 64 at the
+ * least), as in cora_cache_attention (64 rows and query heads of a kv head).  Asynchronous. */
 cora_status cora_cache_store(const cora_cache *cache, int32_t layer, const void *d_x, int32_t x_f32,
                              int64_t ld, int32_t n_heads, const cora_chunk *chunk, int32_t B,
                              const float *d_rope, int32_t n_pos, uint16_t *d_q, void *hip_stream);

@@ -497,23 +497,38 @@ hipError_t launch_rope_rows(const int32_t* positions, const int32_t* cu_end, con
 // 20.9 at 4096, but 15.2 against 14.0 at 2048; of 64, 14.8 against 14.2 at 5120.
 constexpr int64_t MANY_HEADS = 4096;
 
+namespace {
+
+struct StoreGrid {
+  bool many;
+  int64_t workgroups;
+};
+StoreGrid store_grid(int rows, int H, int Hkv, int hd) {
+  const int64_t windows = ((int64_t)rows + 31) / 32;
+  const int hpw = hd == 128 ? 1 : 2;
+  const bool many = hd == 128 && windows * (H + Hkv) >= MANY_HEADS;
+  const int nh = hpw * (many ? 4 : 1);
+  return {many, windows * ((H + Hkv + nh - 1) / nh + (Hkv + hpw - 1) / hpw)};
+}
+
+}  // namespace
+
+int64_t cache_store_workgroups(int rows, int H, int Hkv, int hd) { return store_grid(rows, H, Hkv, hd).workgroups; }
+
 hipError_t launch_cache_store(const CacheStoreArgs& a, int hd, bool paired, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const bool f32 = a.xf != nullptr;
   if (paired && !f32) return hipErrorInvalidValue;
-  const int windows = (int)(((int64_t)a.rows + 31) / 32), hpw = hd == 128 ? 1 : 2;
-  const bool many = hd == 128 && (int64_t)windows * (a.H + a.Hkv) >= MANY_HEADS;
-  const int nh = hpw * (many ? 4 : 1);
-  const int64_t wgs = (int64_t)windows * ((a.H + a.Hkv + nh - 1) / nh + (a.Hkv + hpw - 1) / hpw);
-  if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs);
+  const StoreGrid g = store_grid(a.rows, a.H, a.Hkv, hd);
+  if (g.workgroups > most_workgroups(256)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)g.workgroups);
 #define STORE(HD_, NH_)                                                                                     \
   do {                                                                                                      \
     if (paired) hipLaunchKernelGGL((k_cache_store<HD_, true, true, NH_>), grid, dim3(256), 0, s, a);        \
     else if (f32) hipLaunchKernelGGL((k_cache_store<HD_, true, false, NH_>), grid, dim3(256), 0, s, a);     \
     else hipLaunchKernelGGL((k_cache_store<HD_, false, false, NH_>), grid, dim3(256), 0, s, a);             \
   } while (0)
-  if (many) STORE(128, 4);
+  if (g.many) STORE(128, 4);
   else if (hd == 128) STORE(128, 1);
   else if (hd == 64) STORE(64, 1);
   else return hipErrorInvalidValue;

@@ -738,10 +738,14 @@ CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int 
     p.splits = (int)std::min<int64_t>(std::min(want, by_len), 64);
   }
   const size_t per_split = (size_t)std::max(1, rows) * H * (2 + hd);
-  const int64_t most = std::min<int64_t>(most_ws_floats / per_split, 0x7fffffffLL / units);
+  // the list of work is counted in 31 bits, a grid over all tiles and the merge's over all rows and
+  // heads in workgroups
+  const int64_t list = p.tile_rows <= 32 ? 0x7fffffffLL : most_workgroups(256);
+  int64_t most = std::min<int64_t>(most_ws_floats / per_split, list / units);
+  if (((int64_t)rows * H + 3) / 4 > most_workgroups(256)) most = 1;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.splits, most));
   p.chunk = std::max(64, ((max_len + p.splits - 1) / p.splits + 63) / 64 * 64);
-  p.workgroups = (int)std::min<int64_t>(6 * num_cus, units * p.splits);
+  p.workgroups = (int)std::min<int64_t>(p.tile_rows <= 32 ? 6 * num_cus : 0x7fffffffLL, units * p.splits);
   p.ws_floats = p.splits > 1 ? per_split * p.splits : 0;
   return p;
 }
@@ -756,14 +760,13 @@ hipError_t launch_cache_attention(CacheAttnArgs a, const CacheAttnPlan& p, int h
   if (p.splits > 1 && !ws) return hipErrorInvalidValue;
   a.part_o = ws;
   a.part_ml = ws ? ws + (size_t)a.rows * a.H * p.splits * hd : nullptr;
-  const int64_t wgs = (int64_t)p.tiles * p.splits * a.Hkv;
-  if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)wgs), few((unsigned)p.workgroups);
+  if (p.workgroups > most_workgroups(256)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)p.workgroups);
   const size_t lds = (size_t)(a.B + 1) * 4;
 #define ATTEND(HD_)                                                                                              \
   do {                                                                                                           \
-    if (p.tile_rows == 16) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 1>), few, dim3(256), lds, s, a);         \
-    else if (p.tile_rows == 32) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 2>), few, dim3(256), lds, s, a);    \
+    if (p.tile_rows == 16) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 1>), grid, dim3(256), lds, s, a);        \
+    else if (p.tile_rows == 32) hipLaunchKernelGGL((k_cache_attend_rows<HD_, 2>), grid, dim3(256), lds, s, a);   \
     else if (p.tile_rows == 64) hipLaunchKernelGGL((k_cache_attend_tile<HD_, 1>), grid, dim3(256), 0, s, a);     \
     else hipLaunchKernelGGL((k_cache_attend_tile<HD_, 2>), grid, dim3(256), 0, s, a);                            \
     if (p.splits > 1) {                                                                                          \

@@ -7,6 +7,9 @@
 
 namespace cora {
 
+// Workgroups of a launch, whose threads are counted in 32 bits.
+constexpr int64_t most_workgroups(int threads) { return 0xffffffffLL / threads; }
+
 // ---- sampling -----------------------------------------------------------------------------
 // Row r of the logits starts at logits + r * ld.  top_k, top_p, min_p may be null (off).
 struct SampleArgs {
@@ -17,6 +20,7 @@ struct SampleArgs {
   const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p; const float* u;
   int32_t* token; float* conf;
 };
+constexpr int64_t SAMPLE_MAX_ROWS = most_workgroups(512);  // a workgroup a row, of 1024 threads up to 256 rows
 hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s);
 
 // ---- paged K/V cache -----------------------------------------------------------------------
@@ -57,6 +61,7 @@ struct CacheStoreArgs {
 hipError_t launch_rope_rows(const int32_t* positions, const int32_t* cu_end, const float* table, int n_pos,
                             const double* freq, int rows, int half, float* out, hipStream_t s);
 // paired: a head's dimensions come pair-interleaved (ROW_ROPE_PAIR) and stay so
+int64_t cache_store_workgroups(int rows, int H, int Hkv, int hd);
 hipError_t launch_cache_store(const CacheStoreArgs& a, int hd, bool paired, hipStream_t s);
 struct CacheAttnArgs {
   const uint16_t *q, *k, *v;
@@ -73,7 +78,7 @@ struct CacheAttnArgs {
 struct CacheAttnPlan {
   int tile_rows, tiles, splits, chunk;
   int per_request;  // tiles of each request where they have about as many rows, or 0
-  int workgroups;   // of the few-rows kernel
+  int workgroups;
   size_t ws_floats;
 };
 CacheAttnPlan cache_attention_plan(int B, int rows, int H, int Hkv, int hd, int max_count, int max_len,

@@ -953,7 +953,8 @@ extern "C" cora_status cora_vocab_sample(const uint16_t* d_logits, int32_t R, in
                                          int32_t* d_token, float* d_conf, void* hip_stream) try {
   if (R < 0 || V < 1 || ld < V || mask_id < -1 || mask_id >= V)
     return fail(CORA_ERR_INVALID_ARG, "R >= 0, V >= 1, ld >= V and mask_id in [-1, V)");
-  if (V > (1 << 30)) return fail(CORA_ERR_UNSUPPORTED, "V must not exceed 2^30");
+  if (V > (1 << 30) || R > SAMPLE_MAX_ROWS)
+    return fail(CORA_ERR_UNSUPPORTED, "V must not exceed 2^30, R must stay below 2^23");
   if (R == 0) return CORA_OK;  // no row: the arrays may be null
   if (cora_status e = check_sample_rows(rows)) return e;
   if (!d_logits || !d_token || !d_conf) return fail(CORA_ERR_INVALID_ARG, "null argument");
@@ -970,7 +971,8 @@ extern "C" cora_status cora_vocab_gate_sampled(const uint16_t* d_logits, int32_t
                                                void* hip_stream) try {
   if (cora_status e = check_vocab_gate(d_logits, n_rows, row_begin, V, mask_id, st, sc, gt)) return e;
   if (cora_status e = check_sample_rows(rows)) return e;
-  if ((int64_t)st->B * n_rows > 0x7fffffffLL) return fail(CORA_ERR_UNSUPPORTED, "B * n_rows exceeds 2^31");
+  if ((int64_t)st->B * n_rows > SAMPLE_MAX_ROWS)
+    return fail(CORA_ERR_UNSUPPORTED, "B * n_rows must stay below 2^23");
   const VocabGateArgs a = vg_args(d_logits, n_rows, row_begin, V, mask_id, st, k_transfer, sc, gt);
   HIP_TRY(launch_vocab_sample(sample_args(d_logits, st->B * n_rows, V, V, mask_id, rows, st->top1, st->conf),
                               S(hip_stream)));
@@ -1071,6 +1073,8 @@ extern "C" cora_status cora_cache_store(const cora_cache* cache, int32_t layer, 
     return fail(CORA_ERR_INVALID_ARG, "ld must cover a row and keep rows aligned to 16 bytes");
   if (!aligned16(d_x) || !aligned16(d_rope) || !aligned16(d_q))
     return fail(CORA_ERR_INVALID_ARG, "x, rope and q must be aligned to 16 bytes");
+  if (cache_store_workgroups(c->rows, n_heads, cache->n_kv_heads, hd) > most_workgroups(256))
+    return fail(CORA_ERR_UNSUPPORTED, "rows and heads exceed a launch: use several chunks");
   CacheStoreArgs a{};
   if (x_f32) a.xf = static_cast<const float*>(d_x);
   else a.xb = static_cast<const uint16_t*>(d_x);
@@ -1109,8 +1113,8 @@ extern "C" cora_status cora_cache_attention_workspace(int32_t n_heads, int32_t n
   if (B < 1 || rows < 0 || max_len < 1) return fail(CORA_ERR_INVALID_ARG, "B >= 1, rows >= 0, max_len >= 1");
   if (head_dim != 64 && head_dim != 128) return fail(CORA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
   if (cora_status e = check_heads(n_heads, n_kv_heads, rows)) return e;
-  *bytes = 4 * cache_attention_plan(B, rows, n_heads, n_kv_heads, head_dim, expected(max_count, rows), max_len,
-                                    current_cus(), SIZE_MAX).ws_floats;
+  *bytes = 4 * cache_attention_plan(B, rows, n_heads, n_kv_heads, head_dim, expected(max_count, rows),
+                                    expected(max_len, 1 << 30), current_cus(), SIZE_MAX).ws_floats;
   return CORA_OK;
 } catch (...) {
   return exception_status();
@@ -1137,6 +1141,8 @@ extern "C" cora_status cora_cache_attention(const cora_cache* cache, int32_t lay
       expected(max_len, (int64_t)p->max_pages * p->page_size), current_cus(), SIZE_MAX);
   if (pl.ws_floats && (!workspace || !aligned16(workspace) || workspace_bytes < pl.ws_floats * 4))
     return fail(CORA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than cora_cache_attention_workspace says");
+  if (pl.workgroups > most_workgroups(256))
+    return fail(CORA_ERR_UNSUPPORTED, "rows and heads exceed a launch: use several chunks");
   CacheAttnArgs a{};
   a.q = d_q; a.out = d_out;
   a.k = cache->k + layer * cache_layer_elems(cache);
