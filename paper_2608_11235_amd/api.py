@@ -282,9 +282,11 @@ def _rows_2d(t, name, dtypes):
         raise ValueError(f"{name}: expected two dimensions, [R, V] or [rows, width], got {tuple(t.shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: dtype {t.dtype}, expected one of {dtypes}")
+    n, width = t.shape
+    if n >> 31 or width >> 31:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, sizes must stay below 2^31")
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a GPU tensor (got device {t.device})")
-    n, width = t.shape
     ld, step = t.stride()
     if (width > 1 and step != 1) or (n > 1 and ld < width):
         raise ValueError(f"{name}: strides {t.stride()}, expected rows of stride 1 that do not overlap")

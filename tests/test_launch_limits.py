@@ -2,7 +2,9 @@
 import ctypes
 
 import pytest
+import torch
 
+from paper_2608_11235_amd import api
 from tests.test_cache_abi import FAKE, UNSUPPORTED, attend, cache, chunk, lib, pages, store  # noqa: F401
 
 
@@ -39,3 +41,11 @@ def test_attention_workspace_of_many_rows(lib):  # noqa: F811
 def test_attention_tiles(lib):  # noqa: F811
     big = dict(ca=cache(lib, head_dim=64, n_kv_heads=1 << 13), ch=chunk(lib, rows=1 << 17), heads=1 << 13)
     assert attend(lib, pg=pages(lib, B=4096), count=40, **big) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("shape", [(1 << 31, 1), (1, 1 << 31), ((1 << 32) + 5, 1)])
+def test_binding_refuses_shapes_beyond_32_bits(shape):
+    """The library would take (2^32 + 5) rows for 5."""
+    x = torch.empty(shape, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        api._rows_2d(x, "logits", (torch.bfloat16,))
