@@ -6,7 +6,8 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2608_11235_amd import vocab_sample
+import seeded_inputs as si
+from paper_2608_11235_amd import DecodeState, Gate, Sched, vocab_gate_sampled, vocab_sample
 from tests.gpu_common import log_case, require_gpu
 from tests.test_gpu_sampling import LOWEST, bf16, check_rows, settings
 
@@ -173,3 +174,25 @@ def test_256_and_257_rows_give_the_same(V):
                                   top_p=dev["top_p"][:n], min_p=dev["min_p"][:n])
     (a, ca), (b, cb) = call(256), call(257)
     assert torch.equal(a, b[:256]) and torch.equal(ca, cb[:256])
+
+
+def test_gate_on_a_whole_generation_region():
+    """The rules take these kernels' tokens and confidences too: 3 x 112 rows in GLOBAL scope."""
+    require_gpu()
+    rng = np.random.default_rng(95)
+    B, P, G, blk, V, mask = 3, 5, 112, 16, 1009, 1000
+    R = B * G
+    host = si.initial_decode_state(si.prompt_tokens(1, B, P, V, mask), G, mask)
+    st = DecodeState.from_host(host, P, G, G, blk)
+    logits = bf16(rng.normal(size=(B, G, V)) * 4).cuda()
+    T, u = torch.full((R,), 0.7, device="cuda"), torch.as_tensor(rng.random(R, dtype=np.float32)).cuda()
+    tok, conf = vocab_sample(logits.view(R, V), mask, T, u)
+    vocab_gate_sampled(logits, G, P, V, mask, st, 2, Sched(blk, 8), Gate(0.5, 1, True, 1), T, u)
+    after = st.to_host()
+    tok, conf = tok.cpu().numpy().reshape(B, G), conf.cpu().numpy().reshape(B, G)
+    assert (after["top1"] == tok).all() and (after["conf"] == conf).all()
+    for b in range(B):
+        first = sorted(range(blk), key=lambda p: (-conf[b, p], p))[:2]  # the gate needs a repeated draw
+        want = host["tokens"][b].copy()
+        want[[P + p for p in first]] = tok[b, first]
+        assert (after["tokens"][b] == want).all()
