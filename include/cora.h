@@ -331,7 +331,9 @@ typedef struct {
  * A request is refused, with its state left as it was, no rows and its status set, when start is
  * negative or beyond len, or start + count beyond max_pages * page_size (CORA_ERR_INVALID_ARG);
  * when the pages needed up to it exceed the free ones (CORA_ERR_OOM); or when the rows up to it
- * exceed chunk->rows (CORA_ERR_UNSUPPORTED).  Status 0 otherwise.  reset != 0 forgets every
+ * exceed chunk->rows (CORA_ERR_UNSUPPORTED).  "Up to it" counts what the valid requests before it
+ * asked for, those refused among them, so that no later request overtakes one that waits for pages
+ * or rows; one that needs no page never gets CORA_ERR_OOM.  Status 0 otherwise.  reset != 0 forgets every
  * request first: len 0, all pages free, page 0 handed out first.  B <= CORA_CACHE_MAX_BATCH.
  * Allocates nothing.  Asynchronous. */
 cora_status cora_cache_plan(cora_pages *pages, cora_chunk *chunk, int32_t reset, void *hip_stream);
@@ -352,7 +354,8 @@ cora_status cora_cache_store(const cora_cache *cache, int32_t layer, const void 
 
 /* Attention of the chunk's rows over their requests' pages: query head h reads kv head
  * h / (n_heads / n_kv_heads); keys j < len, and with causal != 0 j <= the row's position.
- * d_q, d_out bf16 [rows, n_heads, head_dim].  A row without a key is zero; rows before cu[0]
+ * d_q, d_out bf16 [rows, n_heads, head_dim].  A row without a key, or whose scores are all -inf, is
+ * zero; rows before cu[0]
  * and from cu[B] on are left alone; what the pages hold behind len is never used.  Read: chunk start, cu; pages
  * table, len.  max_count and max_len are the most rows of a request and the longest len to
  * expect (<= 0: rows and max_pages * page_size); they choose tiles and key ranges, and with

@@ -69,7 +69,7 @@ struct Work {
 // first, and the first range, which holds the short ones whole, fills the gaps at the end.  With
 // `per_request` tiles a request (every request has about as many rows) a workgroup's place follows from
 // its number, the kv head the fastest and the later tiles, which see more keys under the causal mask,
-// before the earlier ones (382 us against 402).  Else (a prompt beside single tokens) tile t belongs to
+// before the earlier ones (4 x 2048 tokens, the kernel's case below: 351 us in either order).  Else (a prompt beside single tokens) tile t belongs to
 // the request b with base_b <= t < base_(b+1), base_b = cu_b G / RT + b, which leaves each request at
 // least as many tiles as it fills and needs no pass over the lengths, and an XCD takes a range of kv
 // heads and tiles, whose keys its L2 then holds.
@@ -192,6 +192,10 @@ __device__ __forceinline__ void soften(f32x4_t (&st)[RB][NB], float scale_log2, 
       }
 }
 
+// The terms of eight keys as the second product's operand.  V is bf16 and the matrix instruction takes
+// both operands in one type, so a term is rounded by up to 2^-8 of it, while its sum l adds the fp32
+// value.  Outputs are off from 64 bits by 2.0e-3 to 2.3e-3 of their norm, 1.7e-3 of which is their own
+// rounding (what fp32 terms leave).  Terms in two bf16 parts would double the second product.
 __device__ __forceinline__ bf16x8_t terms_operand(const f32x4_t& x, const f32x4_t& y) {
   return as_bf16x8(u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(y[0], y[1]),
                            pack_bf16x2(y[2], y[3])});
@@ -506,7 +510,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend_rows(CacheAttnArgs a) {
 
 // Bound by the products and, nearly as much, by the LDS reads that feed them (a fragment of K or V
 // serves RB x 16 rows) and the exponentials: 4 x 2048 tokens of 28 heads of 128 behind 2048 others,
-// causal, 344 us, 1.05 PFLOP/s.  Tiles that no row's limit cuts take a path without masks or branches
+// causal, 345 to 362 us from card to card, 1.00 to 1.05 PFLOP/s.  Tiles that no row's limit cuts take a path without masks or branches
 // but one, for a moved reference.  Tried at RB = 2: 32-key tiles in 2 to 4 stages, two or three
 // workgroups a CU (366 us); RB = 3 (348 us, and 54 against 44 us where 2 x 1024 tokens of 32 heads
 // leave fewer workgroups than places); RB = 4 on one wavefront a SIMD (544 us).

@@ -28,8 +28,8 @@
 // numbers far below the maximum (a ban by bf16's lowest one), whose terms are 0 in 64 bits, do not
 // count.
 //
-// 4096 rows of 126464 take 225 us, 4.6 TB/s.  Three things of like size share that time: the rows'
-// bytes (150 us at the 6.9 TB/s of a plain reading, and up to a third more for step 4), the LDS adds (117 us: 3.7 ns a wavefront's 64
+// 4096 rows of 126464 take 226 us, 4.6 TB/s.  Three things of like size share that time: the rows'
+// bytes (150 us at the 6.9 TB/s of a plain reading, and 22 % more for step 4), the LDS adds (117 us: 3.7 ns a wavefront's 64
 // on a CU when they fall on some 500 words, 1.8 without bank conflicts) and about 7 instructions a
 // logit (95 us).  Steps 2 to 4 are 13 of a row's 32 us, beside two other rows' counting.  A single
 // row is bound by latency: 2048 logits 8 us in the kernel, 126464 17 us, 9 of them counting.
