@@ -463,16 +463,16 @@ def cache_store(cache: KVCache, layer, x, n_heads, chunk: Chunk, rope=None, q=No
     if x.shape[0] < rows or x.shape[1] != width or xdev != device:
         raise ValueError(f"x: shape {tuple(x.shape)} on {x.device}, the call needs [{rows}, {width}] on "
                          f"cuda:{device}")
-    n_pos = 0
+    n_pos, angles = 0, None
     if rope is not None:
-        if rope.dim() != 3 or rope.shape[1:] != (hd // 2, 2):
+        angles = _checked(rope, "rope", _F32, 0, device)
+        if rope.dim() != 3 or rope.shape[0] < 1 or rope.shape[1:] != (hd // 2, 2):
             raise ValueError(f"rope: shape {tuple(rope.shape)}, expected [n_pos, {hd // 2}, 2]")
         n_pos = rope.shape[0]
     if q is None:
         q = _empty((rows, n_heads, hd), torch.bfloat16, x.device, stream)
     _call(device, "cora_cache_store", cache._cache, layer, x.data_ptr(), 1 if x.dtype is torch.float32 else 0,
-          ld, n_heads, chunk._chunk, chunk._batch,
-          None if rope is None else _checked(rope, "rope", _F32, 0, device), n_pos,
+          ld, n_heads, chunk._chunk, chunk._batch, angles, n_pos,
           _checked(q, "q", _BF16_BITS, rows * n_heads * hd, device), stream=stream)
     return q
 
