@@ -387,6 +387,42 @@ cora_status cora_forward_cached(cora_model *model, const cora_cache *cache, cons
                                 int32_t max_count, int32_t max_len, int32_t causal,
                                 uint16_t *d_logits, void *hip_stream);
 
+/* ---- 8-bit rows and their products ---------------------------------------------------------
+ * A matrix [rows, cols] in 8-bit floating point (e4m3: OCP's, without infinities), each 128 columns of
+ * a row with a power of two as their scale.  Device arrays owned by the caller, of
+ * cora_rows_bytes bytes, data aligned to 16 bytes, scale to 4.  With groups of 16 rows, blocks of
+ * 128 columns, nb = ceil(cols / 128) and nq = ceil(cols / 512), element (r, c) is at
+ *   data:  ((r/16) nb + c/128) 2048 + (c%128 / 64) 1024 + (c/16 % 4) 256 + (r%16) 16 + c%16
+ * and its scale, the exponent + 127, at
+ *   scale: ((r/16) nq + c/512) 64 + (r%16) 4 + c/128 % 4.
+ * Rows and columns up to multiples of 16 and 128 are zero, the scales of blocks past the last one 127.
+ * Limits: rows <= 2^27, cols <= 2^20. */
+typedef struct {
+  uint8_t *data, *scale;
+  int32_t rows, cols;
+} cora_rows8;
+cora_status cora_rows_bytes(int32_t rows, int32_t cols, size_t *data_bytes, size_t *scale_bytes);
+
+/* x [rows, cols] to 8 bits, row stride ld (elements, ld >= cols): bf16 (x_f32 = 0, any alignment of 2
+ * bytes) or fp32 (any of 4).  The scale of a block is the least power of two, 2^-127 at the least, with
+ * which 448 reaches the largest finite magnitude in it (1 for a block of zeros); values are x / scale
+ * rounded to e4m3 once, to nearest even.  NaN and infinities become NaN.  Writes the whole arrays, their padding
+ * included.  rows * ceil(cols / 512) stays below 2^27.  Asynchronous. */
+cora_status cora_quantize_rows(const void *d_x, int32_t x_f32, int64_t ld, const cora_rows8 *out,
+                               void *hip_stream);
+
+/* out[m, n] = sum over k of a[m, k] w[n, k], + d_bias[n] (fp32 [N], NULL: none): M = a->rows, N = w->rows, both
+ * of the same cols.  Products are exact, sums fp32, each output rounded once: bf16 (out_f32 = 0) or fp32
+ * [M, N], row stride ld (elements, ld >= N).  Sums over cols are split by sizes alone, so that an output's bits do not
+ * change with what else M and N rows hold.  workspace of cora_rows_product_workspace bytes, 16-byte
+ * aligned (NULL when that is 0): used from this call's start to its end on the stream, contents not
+ * kept; calls that may overlap and captured graphs that may run at once need one each.  cols = 0 is
+ * refused; M = 0 or N = 0 does nothing.  Asynchronous. */
+cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, size_t *bytes);
+cora_status cora_rows_product(const cora_rows8 *a, const cora_rows8 *w, const float *d_bias,
+                               void *d_out, int32_t out_f32, int64_t ld, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
 /* Copy weight tensor `tensor_id` (ids as in cora_model_create) to host memory
  * in its logical row-major [out, in] layout as bf16 bits (biases too).
  * `bytes` must equal the tensor's size.  Synchronous. */

@@ -60,6 +60,10 @@ class ChunkRows(ctypes.Structure):
                 ("slots", c_vp), ("status", c_vp), ("rows", c_i32)]
 
 
+class Rows8(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("scale", c_vp), ("rows", c_i32), ("cols", c_i32)]
+
+
 _P = ctypes.POINTER
 
 EXPORTS = {
@@ -88,6 +92,10 @@ EXPORTS = {
                                      c_i32, c_i32, c_f32, c_vp, c_vp, c_sz, c_vp]),
     "cora_forward_cached": (c_i32, [c_vp, _P(Cache), _P(Pages), _P(ChunkRows), c_vp, c_i32, c_i32,
                                     c_i32, c_vp, c_vp]),
+    "cora_rows_bytes": (c_i32, [c_i32, c_i32, _P(c_sz), _P(c_sz)]),
+    "cora_quantize_rows": (c_i32, [c_vp, c_i32, c_i64, _P(Rows8), c_vp]),
+    "cora_rows_product_workspace": (c_i32, [c_i32, c_i32, c_i32, _P(c_sz)]),
+    "cora_rows_product": (c_i32, [_P(Rows8), _P(Rows8), c_vp, c_vp, c_i32, c_i64, c_vp, c_sz, c_vp]),
     "cora_model_copy_tensor": (c_i32, [c_vp, c_i32, c_vp, c_sz]),
     "cora_model_set_timing": (c_i32, [c_vp, c_i32]),
     "cora_model_set_compaction": (c_i32, [c_vp, c_i32]),

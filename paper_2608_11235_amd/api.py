@@ -518,3 +518,102 @@ def cache_attention(cache: KVCache, layer, q, chunk: Chunk, max_count=0, max_len
           None if workspace is None else _checked(workspace, "workspace", _U8, 0, device),
           0 if workspace is None else workspace.numel(), stream=stream)
     return out
+
+
+# ---- 8-bit rows and their products ----------------------------------------------------------------
+@_fixed("data", "scale", "rows", "cols")
+class Rows8:
+    """A matrix [rows, cols] in 8-bit floating point, each 128 columns of a row with a power of two as
+    their scale, in the order of the products' operands (cora_rows8).  Zeros at first.  `data` and `scale`
+    are its own for good (written in place, never replaced)."""
+
+    def __init__(self, rows, cols, device="cuda"):
+        data, scale = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        check(_lib.load().cora_rows_bytes(rows, cols, ctypes.byref(data), ctypes.byref(scale)), "cora_rows_bytes")
+        self._hold(rows, cols, torch.zeros(data.value, dtype=torch.uint8, device=device),
+                   torch.full((scale.value,), 127, dtype=torch.uint8, device=device))
+
+    def _hold(self, rows, cols, data, scale):
+        self._rows, self._cols, self._data, self._scale = rows, cols, data, scale
+        self._device = data.get_device()
+        self._c = ctypes.byref(_lib.Rows8(data.data_ptr(), scale.data_ptr(), rows, cols))
+        return self
+
+    @classmethod
+    def _empty(cls, rows, cols, device, stream):
+        """For a call that writes all of it."""
+        groups = (rows + 15) // 16
+        return cls.__new__(cls)._hold(
+            rows, cols, _empty(groups * ((cols + 127) // 128) * 2048, torch.uint8, device, stream),
+            _empty(groups * ((cols + 511) // 512) * 64, torch.uint8, device, stream))
+
+    def values(self):
+        """The numbers that the rows stand for, float32 [rows, cols]."""
+        groups, blocks = -(-self._rows // 16), -(-self._cols // 128)
+        q = self._data.view(torch.float8_e4m3fn).double().view(groups, blocks, 8, 16, 16)
+        s = self._scale.view(groups, -1, 16, 4).transpose(2, 3).reshape(groups, -1, 1, 16, 1)[:, :blocks]
+        x = torch.ldexp(q, s.int() - 127).float().permute(0, 3, 1, 2, 4)  # in 64 bits: 2^-127 is no normal float32
+        return x.reshape(groups * 16, blocks * 128)[:self._rows, :self._cols].contiguous()
+
+
+def quantize_rows(x, out=None, stream=None):
+    """The rows of x [rows, cols] (bf16 or float32, rows may be strided) in 8 bits (cora_quantize_rows);
+    returns a Rows8."""
+    device, ld = _rows_2d(x, "x", _STORED)
+    rows, cols = x.shape
+    if out is None:
+        if cols < 1:
+            raise ValueError(f"x: shape {tuple(x.shape)}, at least one column is needed")
+        out = Rows8._empty(rows, cols, x.device, stream)
+    elif (out._rows, out._cols, out._device) != (rows, cols, device):
+        raise ValueError(f"out: [{out._rows}, {out._cols}] on cuda:{out._device}, x is {tuple(x.shape)} on cuda:{device}")
+    _call(device, "cora_quantize_rows", x.data_ptr(), 1 if x.dtype is torch.float32 else 0, ld, out._c, stream=stream)
+    return out
+
+
+_product_workspaces = {}  # bytes that rows8_product needs, by its sizes
+
+
+def rows8_product_workspace(a: Rows8, w: Rows8):
+    """Bytes of workspace that rows8_product needs for these sizes."""
+    if a._device < 0 or a._device != w._device:
+        raise ValueError("a, w: must be on one GPU")
+    n = ctypes.c_size_t(0)
+    with torch.cuda.device(a._device):
+        check(_lib.load().cora_rows_product_workspace(a._rows, w._rows, a._cols, ctypes.byref(n)),
+              "cora_rows_product_workspace")
+    return n.value
+
+
+def rows8_product(a: Rows8, w: Rows8, bias=None, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+    """a [M, K] times the rows of w [N, K], + bias float32 [N] (cora_rows_product): [M, N] in `dtype`, bf16 or
+    float32, or in `out` (rows may be strided).  workspace: a uint8 tensor of rows8_product_workspace bytes; by
+    default torch's allocator provides one for the call."""
+    device = a._device
+    if device < 0 or w._device != device:
+        raise ValueError(f"w: on cuda:{w._device}, a is on cuda:{device}; both must be on one GPU")
+    if a._cols != w._cols:
+        raise ValueError(f"w: {w._cols} columns, a has {a._cols}")
+    M, N = a._rows, w._rows
+    if out is None:
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"dtype: {dtype}, expected torch.bfloat16 or torch.float32")
+        out, ld = _empty((M, N), dtype, a._data.device, stream), N
+    else:
+        odev, ld = _rows_2d(out, "out", _STORED)
+        if out.shape != (M, N) or odev != device:
+            raise ValueError(f"out: shape {tuple(out.shape)} on {out.device}, the call needs [{M}, {N}] on cuda:{device}")
+    if workspace is None:
+        key = (M, N, a._cols, device)
+        n = _product_workspaces.get(key)
+        if n is None:
+            if len(_product_workspaces) >= 256:
+                _product_workspaces.clear()
+            n = _product_workspaces[key] = rows8_product_workspace(a, w)
+        if n:
+            workspace = _empty(n, torch.uint8, out.device, stream)
+    _call(device, "cora_rows_product", a._c, w._c, None if bias is None else _checked(bias, "bias", _F32, N, device),
+          out.data_ptr(), 1 if out.dtype is torch.float32 else 0, ld,
+          None if workspace is None else _checked(workspace, "workspace", _U8, 0, device),
+          0 if workspace is None else workspace.numel(), stream=stream)
+    return out

@@ -16,6 +16,7 @@
 #include "common.hpp"
 #include "cached.hpp"
 #include "internal.hpp"
+#include "rows8.hpp"
 
 using namespace cora;
 
@@ -1214,6 +1215,86 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
   }
   const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
   return lm_head(m, all, M, M, d_logits, s);
+} catch (...) {
+  return exception_status();
+}
+
+// ---- 8-bit rows -------------------------------------------------------------------------------
+static cora_status check_rows8_sizes(int32_t rows, int32_t cols) {
+  if (rows < 0 || cols < 1) return fail(CORA_ERR_INVALID_ARG, "rows >= 0 and cols >= 1");
+  if (rows > R8_MAX_ROWS || cols > R8_MAX_COLS)
+    return fail(CORA_ERR_UNSUPPORTED, "rows must not exceed 2^27, cols 2^20");
+  return CORA_OK;
+}
+
+static cora_status check_rows8(const cora_rows8* x) {
+  if (!x) return fail(CORA_ERR_INVALID_ARG, "null rows8");
+  if (cora_status e = check_rows8_sizes(x->rows, x->cols)) return e;
+  if (x->rows == 0) return CORA_OK;  // no row: the arrays may be null
+  if (!x->data || !x->scale || !aligned16(x->data) || (reinterpret_cast<uintptr_t>(x->scale) & 3) != 0)
+    return fail(CORA_ERR_INVALID_ARG, "rows8 data and scale must be given, aligned to 16 and 4 bytes");
+  return CORA_OK;
+}
+
+extern "C" cora_status cora_rows_bytes(int32_t rows, int32_t cols, size_t* data_bytes, size_t* scale_bytes) try {
+  if (!data_bytes || !scale_bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
+  if (cora_status e = check_rows8_sizes(rows, cols)) return e;
+  *data_bytes = (size_t)r8_groups(rows) * r8_blocks(cols) * R8_BLOCK;
+  *scale_bytes = (size_t)r8_groups(rows) * r8_quads(cols) * 64;
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_quantize_rows(const void* d_x, int32_t x_f32, int64_t ld, const cora_rows8* out,
+                                          void* hip_stream) try {
+  if (cora_status e = check_rows8(out)) return e;
+  if (out->rows == 0) return CORA_OK;
+  if (!d_x || ld < out->cols || (reinterpret_cast<uintptr_t>(d_x) & (x_f32 ? 3 : 1)) != 0)
+    return fail(CORA_ERR_INVALID_ARG, "x must be given, aligned to its elements, ld >= cols");
+  if ((int64_t)out->rows * r8_quads(out->cols) >= 1 << 27)
+    return fail(CORA_ERR_UNSUPPORTED, "rows * ceil(cols / 512) must stay below 2^27");
+  HIP_TRY(launch_quantize_rows(QuantizeArgs{d_x, ld, out->rows, out->cols, out->data, out->scale}, x_f32 != 0, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+static cora_status check_product_sizes(int32_t M, int32_t N, int32_t cols) {
+  if (cora_status e = check_rows8_sizes(M, cols)) return e;
+  if (cora_status e = check_rows8_sizes(N, cols)) return e;
+  if (M > R8_MAX_PRODUCT_ROWS || N > R8_MAX_PRODUCT_COLS)
+    return fail(CORA_ERR_UNSUPPORTED, "a product's M must not exceed 2^21, its N 2^25");
+  return CORA_OK;
+}
+
+extern "C" cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, size_t* bytes) try {
+  if (!bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
+  if (cora_status e = check_product_sizes(M, N, cols)) return e;
+  *bytes = 4 * rows8_plan(M, N, cols, current_cus()).ws_floats;
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_rows_product(const cora_rows8* a, const cora_rows8* w, const float* d_bias, void* d_out,
+                                          int32_t out_f32, int64_t ld, void* workspace, size_t workspace_bytes,
+                                          void* hip_stream) try {
+  if (cora_status e = check_rows8(a)) return e;
+  if (cora_status e = check_rows8(w)) return e;
+  if (a->cols != w->cols) return fail(CORA_ERR_INVALID_ARG, "a and w differ in cols");
+  const int M = a->rows, N = w->rows;
+  if (cora_status e = check_product_sizes(M, N, a->cols)) return e;
+  if (M == 0 || N == 0) return CORA_OK;
+  if (!d_out || ld < N || (reinterpret_cast<uintptr_t>(d_out) & (out_f32 ? 3 : 1)) != 0 ||
+      (reinterpret_cast<uintptr_t>(d_bias) & 3) != 0)
+    return fail(CORA_ERR_INVALID_ARG, "out must be given, ld >= N, out and bias aligned to their elements");
+  const Rows8Plan pl = rows8_plan(M, N, a->cols, current_cus());
+  if (pl.ws_floats && (!workspace || !aligned16(workspace) || workspace_bytes < pl.ws_floats * 4))
+    return fail(CORA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than cora_rows_product_workspace says");
+  const Rows8ProductArgs g{a->data, a->scale, w->data, w->scale, M, N, a->cols, d_bias, d_out, ld};
+  HIP_TRY(launch_rows8_product(g, pl, out_f32 != 0, static_cast<float*>(workspace), S(hip_stream)));
+  return CORA_OK;
 } catch (...) {
   return exception_status();
 }
