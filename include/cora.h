@@ -284,6 +284,28 @@ cora_status cora_vocab_gate_sampled(const uint16_t *d_logits, int32_t n_rows, in
                                     const cora_gate_cfg *gate, const cora_sample_rows *rows,
                                     void *hip_stream);
 
+/* ---- Beam search --------------------------------------------------------------------------
+ * The W best continuations of each of B requests of K beams.  Row r = b K + k of the bf16 logits
+ * [B K, V] (row stride ld, any alignment of 2 bytes) and d_score float [B K] are beam k of request b and
+ * its running score.  The candidates of a beam are its allowed ids v (not mask_id, not -inf) with
+ *   score + l_v - log sum_u exp(l_u)    over the allowed u;
+ * a beam with d_done != 0 (uint8 [B K], NULL: none) has the one candidate done_token with its score
+ * unchanged.  A beam whose score is -inf, +inf or NaN has none, nor has one without an allowed id or with a NaN or
+ * +inf at one.  In the order of falling scores, equal ones by beam, then by falling logit, then by id,
+ * the first W of a request go to d_token, d_parent (the row r) and d_next (the score) [B, W]; places
+ * left over get token -1, parent -1 and -inf.  Sums and scores are 64-bit beyond a thread's own terms, so that the
+ * order is that of the numbers to about 1e-7.  mask_id = -1: no id is left out.  1 <= K, W <= CORA_BEAM_MAX,
+ * V <= 2^30, B K <= 2^22.  The outputs overlap no input.
+ * workspace of cora_vocab_beam_workspace bytes, 16-byte aligned: used from this call's start to its end on the
+ * stream, contents not kept; calls that may overlap and captured graphs that may run at once need one
+ * each.  Asynchronous. */
+#define CORA_BEAM_MAX 64
+cora_status cora_vocab_beam_workspace(int32_t B, int32_t K, int32_t V, int32_t W, size_t *bytes);
+cora_status cora_vocab_beam(const uint16_t *d_logits, int32_t B, int32_t K, int32_t V, int64_t ld,
+                            int32_t mask_id, const float *d_score, const uint8_t *d_done,
+                            int32_t done_token, int32_t W, int32_t *d_token, int32_t *d_parent,
+                            float *d_next, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* ---- Paged K/V cache ----------------------------------------------------------------------
  * Keeps the K and V of resolved positions, so that a step runs on a chunk of positions per
  * request (its active block, a piece of its prompt, one token) instead of the whole canvas.

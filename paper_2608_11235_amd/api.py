@@ -263,6 +263,7 @@ def vocab_gate_noalloc(logits, n_rows, row_begin, V, mask_id, state: DecodeState
 # These calls take microseconds, so their checks test everything in one expression and look for
 # the message only when it fails.
 _F32, _I32, _U8 = (torch.float32,), (torch.int32,), (torch.uint8,)
+_FLAGS = (torch.uint8, torch.bool)
 
 
 def _checked(t, name, dtypes, numel, device):
@@ -518,6 +519,58 @@ def cache_attention(cache: KVCache, layer, q, chunk: Chunk, max_count=0, max_len
           None if workspace is None else _checked(workspace, "workspace", _U8, 0, device),
           0 if workspace is None else workspace.numel(), stream=stream)
     return out
+
+
+# ---- beam search ------------------------------------------------------------------------------------
+_beam_workspaces = {}  # bytes that vocab_beam needs, by its sizes
+
+
+def vocab_beam_workspace(batch, beams, vocab, width, device=None):
+    """Bytes of workspace that vocab_beam needs for these sizes."""
+    n = ctypes.c_size_t(0)
+    with torch.cuda.device(device):
+        check(_lib.load().cora_vocab_beam_workspace(batch, beams, vocab, width, ctypes.byref(n)),
+              "cora_vocab_beam_workspace")
+    return n.value
+
+
+def vocab_beam(logits, beams, mask_id, score, width=None, done=None, done_token=-1, token=None, parent=None,
+               next_score=None, workspace=None, stream=None):
+    """The `width` (default: beams) best continuations of each request's beams (cora_vocab_beam).
+
+    logits bf16 [B * beams, V], a request's beams one after another, rows may be strided; score float32 of each
+    beam; done uint8 or bool of each beam or None: a finished beam goes on as done_token with its score.  Returns
+    (token int32, parent int32, next_score float32), each [B, width]; parent is the logits row (-1, with
+    token -1 and score -inf, where there are fewer candidates), as cache_reorder takes it.  workspace: a uint8
+    tensor of vocab_beam_workspace bytes; by default torch's allocator provides one for the call."""
+    device, ld = _rows_2d(logits, "logits", _BF16_BITS)
+    R, V = logits.shape
+    if beams < 1 or R % beams:
+        raise ValueError(f"logits: {R} rows, expected a multiple of {beams} beams")
+    B, W = R // beams, beams if width is None else width
+    if W < 1:
+        raise ValueError(f"width: {W}, at least one is needed")
+    if token is None:
+        token = _empty((B, W), torch.int32, logits.device, stream)
+    if parent is None:
+        parent = _empty((B, W), torch.int32, logits.device, stream)
+    if next_score is None:
+        next_score = _empty((B, W), torch.float32, logits.device, stream)
+    if workspace is None:
+        key = (B, beams, V, W, device)
+        n = _beam_workspaces.get(key)
+        if n is None:
+            if len(_beam_workspaces) >= 256:
+                _beam_workspaces.clear()
+            n = _beam_workspaces[key] = vocab_beam_workspace(B, beams, V, W, device)
+        workspace = _empty(n, torch.uint8, logits.device, stream)
+    _call(device, "cora_vocab_beam", logits.data_ptr(), B, beams, V, ld, mask_id,
+          _checked(score, "score", _F32, R, device),
+          None if done is None else _checked(done, "done", _FLAGS, R, device), done_token, W,
+          _checked(token, "token", _I32, B * W, device), _checked(parent, "parent", _I32, B * W, device),
+          _checked(next_score, "next_score", _F32, B * W, device),
+          _checked(workspace, "workspace", _U8, 0, device), workspace.numel(), stream=stream)
+    return token, parent, next_score
 
 
 # ---- 8-bit rows and their products ----------------------------------------------------------------

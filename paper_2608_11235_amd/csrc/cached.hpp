@@ -23,6 +23,29 @@ struct SampleArgs {
 constexpr int64_t SAMPLE_MAX_ROWS = most_workgroups(512);  // a workgroup a row, of 1024 threads up to 256 rows
 hipError_t launch_vocab_sample(const SampleArgs& a, hipStream_t s);
 
+// ---- beams --------------------------------------------------------------------------------
+// Rows of a request's K beams one after another; row r starts at logits + r * ld.  done may be null.
+struct BeamArgs {
+  const uint16_t* logits;
+  int B, K, V;
+  int64_t ld;
+  int mask_id;  // -1: none
+  const float* score; const uint8_t* done;
+  int done_token, W;
+  int32_t *token, *parent; float* next;  // [B][W]
+  int parts, chunk;                      // set by the launcher: a row in `parts` ranges of `chunk` ids
+  double* stats;                         // of each range: a power of two and the sum of exp relative to it
+  uint64_t* best;                        // and its W largest logits
+};
+struct BeamPlan {
+  int parts, chunk;
+  size_t bytes;
+};
+constexpr int64_t BEAM_MAX_ROWS = 1 << 22;  // a workgroup of 512 threads a row and range
+constexpr int BEAM_MAX = CORA_BEAM_MAX;  // beams of a request, and candidates kept of it
+BeamPlan beam_plan(int B, int K, int V, int W, int num_cus);
+hipError_t launch_vocab_beam(BeamArgs a, const BeamPlan& p, void* ws, hipStream_t s);
+
 // ---- paged K/V cache -----------------------------------------------------------------------
 // A page of one kv head holds K and V of its positions as 32-key groups of 1 KB blocks, each the
 // operand of one 16x16x32 MFMA in lane order (lane r + 16 g, 8 elements a lane).

@@ -1219,6 +1219,45 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
   return exception_status();
 }
 
+// ---- beams -----------------------------------------------------------------------------------
+static cora_status check_beam_sizes(int32_t B, int32_t K, int32_t V, int32_t W) {
+  if (B < 0 || K < 1 || W < 1 || V < 1) return fail(CORA_ERR_INVALID_ARG, "B >= 0, K, W and V >= 1");
+  if (K > BEAM_MAX || W > BEAM_MAX) return fail(CORA_ERR_UNSUPPORTED, "K and W must not exceed CORA_BEAM_MAX (64)");
+  if (V > (1 << 30) || (int64_t)B * K > BEAM_MAX_ROWS)
+    return fail(CORA_ERR_UNSUPPORTED, "V must not exceed 2^30, B * K 2^22");
+  return CORA_OK;
+}
+
+extern "C" cora_status cora_vocab_beam_workspace(int32_t B, int32_t K, int32_t V, int32_t W, size_t* bytes) try {
+  if (!bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
+  if (cora_status e = check_beam_sizes(B, K, V, W)) return e;
+  *bytes = beam_plan(B, K, V, W, current_cus()).bytes;
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_vocab_beam(const uint16_t* d_logits, int32_t B, int32_t K, int32_t V, int64_t ld,
+                                       int32_t mask_id, const float* d_score, const uint8_t* d_done,
+                                       int32_t done_token, int32_t W, int32_t* d_token, int32_t* d_parent,
+                                       float* d_next, void* workspace, size_t workspace_bytes, void* hip_stream) try {
+  if (cora_status e = check_beam_sizes(B, K, V, W)) return e;
+  if (ld < V || mask_id < -1 || mask_id >= V) return fail(CORA_ERR_INVALID_ARG, "ld >= V and mask_id in [-1, V)");
+  if (B == 0) return CORA_OK;  // no row: the arrays may be null
+  if (!d_logits || !d_score || !d_token || !d_parent || !d_next) return fail(CORA_ERR_INVALID_ARG, "null argument");
+  const BeamPlan pl = beam_plan(B, K, V, W, current_cus());
+  if (!workspace || !aligned16(workspace) || workspace_bytes < pl.bytes)
+    return fail(CORA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than cora_vocab_beam_workspace says");
+  BeamArgs a{};
+  a.logits = d_logits; a.B = B; a.K = K; a.V = V; a.ld = ld; a.mask_id = mask_id;
+  a.score = d_score; a.done = d_done; a.done_token = done_token; a.W = W;
+  a.token = d_token; a.parent = d_parent; a.next = d_next;
+  HIP_TRY(launch_vocab_beam(a, pl, workspace, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
 // ---- 8-bit rows -------------------------------------------------------------------------------
 static cora_status check_rows8_sizes(int32_t rows, int32_t cols) {
   if (rows < 0 || cols < 1) return fail(CORA_ERR_INVALID_ARG, "rows >= 0 and cols >= 1");
