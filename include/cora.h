@@ -331,6 +331,7 @@ typedef struct {
 typedef struct {
   int32_t *table, *len, *free, *n_free;
   int32_t B, max_pages, n_pages, page_size;
+  int32_t *refs; /* int32 [n_pages]: requests that hold each page, 0 at the start; NULL: no page has two */
 } cora_pages;
 
 /* A chunk per request: positions [start, start + count) of each, their rows one request after
@@ -355,10 +356,27 @@ typedef struct {
  * when the pages needed up to it exceed the free ones (CORA_ERR_OOM); or when the rows up to it
  * exceed chunk->rows (CORA_ERR_UNSUPPORTED).  "Up to it" counts what the valid requests before it
  * asked for, those refused among them, so that no later request overtakes one that waits for pages
- * or rows; one that needs no page never gets CORA_ERR_OOM.  Status 0 otherwise.  reset != 0 forgets every
+ * or rows; one that needs no page never gets CORA_ERR_OOM.  Status 0 otherwise.  With refs (cora_cache_reorder),
+ * a page given back is free once nobody holds it, after those of the requests before the lowest one that
+ * gave it back, and a chunk that reaches into a cached page which another request holds too is refused with
+ * CORA_ERR_STATE.  reset != 0 forgets every
  * request first: len 0, all pages free, page 0 handed out first.  B <= CORA_CACHE_MAX_BATCH.
  * Allocates nothing.  Asynchronous. */
 cora_status cora_cache_plan(cora_pages *pages, cora_chunk *chunk, int32_t reset, void *hip_stream);
+
+/* Every request goes on as its parent: request j gets the positions, K and V that request d_parent[j] (int32
+ * [B], -1: none, request j becomes empty) had before the call.  Full pages are shared: pages->refs
+ * (needed) counts the requests that hold each.  A last page that is not full stays with the parent's lowest
+ * child, the others get copies of it in all layers, 32 positions at a time, in pages off the stack in the
+ * order of the requests; where none is left, a request becomes empty with status CORA_ERR_OOM, and so do
+ * those behind it that need one.  Before that, the pages that nobody holds any more go onto the stack, in the
+ * order of the requests that held them, a page of several at its lowest one's.  A parent outside [-1, B) leaves a
+ * request as it is, as its own child, with status CORA_ERR_INVALID_ARG.  Status int32 [B] is 0 otherwise.  d_moves int32
+ * [1 + 3 B] receives the number of copies and each one's source, destination and 32-position groups.  What the
+ * table holds behind a request's pages stays.  A slot map made before the call is not valid after it.  Allocates
+ * nothing.  Asynchronous. */
+cora_status cora_cache_reorder(const cora_cache *cache, cora_pages *pages, const int32_t *d_parent,
+                               int32_t *d_status, int32_t *d_moves, void *hip_stream);
 
 /* Write a chunk's K and V into the pages of one layer, q and k rotated (rotate-half RoPE: pair
  * (j, j + hd/2) of a head by the angle of the row's position).  d_x rows [q | k | v] of

@@ -14,6 +14,7 @@ supplies device memory and the HIP stream only.
                                             paged K/V cache and attention of a chunk over it
     Model.forward_cached(cache, chunk, tokens)
     vocab_beam(logits, beams, ...)          the best continuations of a request's beams
+    cache_reorder(cache, parent)            the cache's requests go on as their parents, pages shared
     Rows8, quantize_rows, rows8_product     matrices in 8 bits, a power of two as the scale of each 128
                                             columns of a row, and their products
 """
@@ -21,7 +22,7 @@ from .api import (  # noqa: F401
     Model, DecodeState, Sched, Gate, vocab_gate, vocab_gate_noalloc, model_cfg_from,
     vocab_sample, vocab_gate_sampled, KVCache, Chunk, cache_plan, cache_store, cache_attention,
     cache_attention_workspace, rope_table, Rows8, quantize_rows, rows8_product, rows8_product_workspace,
-    vocab_beam, vocab_beam_workspace,
+    vocab_beam, vocab_beam_workspace, cache_reorder,
     TENSOR_EMBED, TENSOR_LM_HEAD, layer_tensor_id,
 )
 from .configs import TINY, LLADA_8B, DREAM_7B, ModelConfig  # noqa: F401

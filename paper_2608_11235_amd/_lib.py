@@ -52,7 +52,7 @@ class Cache(ctypes.Structure):
 
 class Pages(ctypes.Structure):
     _fields_ = [("table", c_vp), ("len", c_vp), ("free", c_vp), ("n_free", c_vp), ("B", c_i32),
-                ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32)]
+                ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32), ("refs", c_vp)]
 
 
 class ChunkRows(ctypes.Structure):
@@ -92,6 +92,7 @@ EXPORTS = {
                                      c_i32, c_i32, c_f32, c_vp, c_vp, c_sz, c_vp]),
     "cora_forward_cached": (c_i32, [c_vp, _P(Cache), _P(Pages), _P(ChunkRows), c_vp, c_i32, c_i32,
                                     c_i32, c_vp, c_vp]),
+    "cora_cache_reorder": (c_i32, [_P(Cache), _P(Pages), c_vp, c_vp, c_vp, c_vp]),
     "cora_vocab_beam_workspace": (c_i32, [c_i32, c_i32, c_i32, c_i32, _P(c_sz)]),
     "cora_vocab_beam": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i64, c_i32, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp,
                                 c_vp, c_sz, c_vp]),

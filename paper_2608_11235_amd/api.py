@@ -376,15 +376,16 @@ def _fixed(*names):
     return add
 
 
-@_fixed("k", "v", "table", "len", "free", "n_free", "n_layers", "n_pages", "n_kv_heads", "head_dim",
+@_fixed("k", "v", "table", "len", "free", "n_free", "refs", "n_layers", "n_pages", "n_kv_heads", "head_dim",
         "page_size", "batch", "max_pages")
 class KVCache:
     """Paged K and V of n_layers layers and the pages that up to `batch` requests hold of them
-    (cora_cache and cora_pages in include/cora.h).  Starts empty, all pages free.  Its tensors are
-    its own for good (written in place, never replaced)."""
+    (cora_cache and cora_pages in include/cora.h).  Starts empty, all pages free.  shared: its requests may
+    hold pages together (cache_reorder).  Its tensors are its own for good (written in place, never
+    replaced)."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, page_size, batch, max_pages,
-                 device="cuda"):
+                 device="cuda", shared=False):
         self._n_layers, self._n_pages, self._n_kv_heads = n_layers, n_pages, n_kv_heads
         self._head_dim, self._page_size, self._batch, self._max_pages = head_dim, page_size, batch, max_pages
         shape = (n_layers, n_pages, n_kv_heads, page_size * head_dim)
@@ -395,13 +396,15 @@ class KVCache:
         self._len = torch.zeros(batch, dtype=i32, device=device)
         self._free = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=device)
         self._n_free = torch.full((1,), n_pages, dtype=i32, device=device)
+        self._refs = torch.zeros(n_pages, dtype=i32, device=device) if shared else None
         self._device = self._k.get_device()
         self._workspaces = {}  # bytes that cache_attention needs, by its sizes
         self._cache = ctypes.byref(_lib.Cache(self._k.data_ptr(), self._v.data_ptr(), n_layers, n_pages,
                                               n_kv_heads, page_size, head_dim))
         self._pages = ctypes.byref(_lib.Pages(self._table.data_ptr(), self._len.data_ptr(),
                                               self._free.data_ptr(), self._n_free.data_ptr(), batch,
-                                              max_pages, n_pages, page_size))
+                                              max_pages, n_pages, page_size,
+                                              self._refs.data_ptr() if shared else None))
 
 
 @_fixed("start", "count", "cu", "positions", "slots", "status", "batch", "rows")
@@ -440,6 +443,25 @@ def cache_plan(cache: KVCache, chunk: Chunk, reset=False, stream=None):
     """Pages for the chunk and its rows' positions and slots (cora_cache_plan)."""
     _call(_device_of(cache, chunk), "cora_cache_plan", cache._pages, chunk._chunk, 1 if reset else 0,
           stream=stream)
+
+
+def cache_reorder(cache: KVCache, parent, status=None, moves=None, stream=None):
+    """Request j goes on as request parent[j] (int32 [batch], -1: as an empty one) of a cache made with
+    shared=True: full pages are shared, the last one is copied where several go on with it
+    (cora_cache_reorder).  Returns status int32 [batch]; moves int32 [1 + 3 batch] receives the copies made."""
+    device = cache._device
+    if device < 0:
+        raise ValueError("cache: must be on a GPU")
+    if cache._refs is None:
+        raise ValueError("cache: made without shared=True")
+    B = cache._batch
+    if status is None:
+        status = _empty(B, torch.int32, cache._k.device, stream)
+    if moves is None:
+        moves = _empty(1 + 3 * B, torch.int32, cache._k.device, stream)
+    _call(device, "cora_cache_reorder", cache._cache, cache._pages, _checked(parent, "parent", _I32, B, device),
+          _checked(status, "status", _I32, B, device), _checked(moves, "moves", _I32, 1 + 3 * B, device), stream=stream)
+    return status
 
 
 def rope_table(n_pos, head_dim, theta, device="cuda"):

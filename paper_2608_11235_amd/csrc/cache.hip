@@ -74,6 +74,59 @@ __device__ __forceinline__ void owners(const uint32_t* first, int B, uint32_t i,
   }
 }
 
+// ---- pages with several holders -------------------------------------------------------------------------
+// Counts are changed and read where the atomics are, behind the first cache.
+__device__ __forceinline__ int count_of(const int32_t* refs, int page) {
+  return __hip_atomic_load(refs + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void set_count(int32_t* refs, int page, int n) {
+  __hip_atomic_store(refs + page, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// every wavefront's changes of counts have arrived there
+__device__ __forceinline__ void settled_barrier() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Page entries [0, total) of the requests (entry i belongs to the last b with first[b] <= i) that their
+// requests let go of; refs has been lowered.  Those that nobody holds go onto the stack in the order of
+// the entries, each from its lowest request, which the others learn through the count itself: below
+// zero it is INT_MIN + that request.  Returns their number.
+template <class Drops>
+__device__ __forceinline__ int push_unheld(const int32_t* table, int32_t* refs, int32_t* free, int B, int max_pages, int n_pages,
+                                           int n_free, const uint32_t* first, uint32_t total, Drops&& drops,
+                                           uint32_t (*part)[PT / 64]) {
+  auto entry = [&](uint32_t i, int& b) {
+    b = owner(first, B, i);
+    if (!drops(b)) return -1;
+    const int page = table[(int64_t)b * max_pages + (i - first[b])];
+    return (uint32_t)page < (uint32_t)n_pages ? page : -1;
+  };
+  settled_barrier();
+  for (uint32_t i = threadIdx.x; i < total; i += PT) {
+    int b;
+    const int page = entry(i, b);
+    if (page >= 0 && count_of(refs, page) <= 0) atomicMin(refs + page, INT_MIN + b);
+  }
+  settled_barrier();
+  uint32_t carry[2] = {0, 0};
+  const uint32_t room = (uint32_t)(n_pages - n_free);
+  for (uint32_t i0 = 0; i0 < total; i0 += PT) {
+    const uint32_t i = i0 + threadIdx.x;
+    int b = 0;
+    const int page = i < total ? entry(i, b) : -1;
+    const bool gives = page >= 0 && count_of(refs, page) == INT_MIN + b;
+    uint32_t v[2] = {gives ? 1u : 0u, 0};
+    block_scan(v, carry, part);
+    if (gives) {
+      if (v[0] <= room) free[n_free + (int)v[0] - 1] = page;
+      set_count(refs, page, 0);
+    }
+  }
+  settled_barrier();
+  return (int)min(carry[0], room);  // more only if a table holds a page twice
+}
+
 __device__ __forceinline__ int pages_of(int len, int shift) { return (int)(((int64_t)len + (1 << shift) - 1) >> shift); }
 
 // Positions and slots of rows r .. r + 3.  `top` != null: the pages that the call takes are read from
@@ -113,6 +166,7 @@ __device__ __forceinline__ void place_rows(const CachePlanArgs& a, const uint32_
 // read back.  64 requests of one token 4.8 us (a search of
 // its own for every page and row, scans by lane exchanges through LDS: 6.0); 512 prompts of 545
 // thousand rows 7.9 us (13.0) and 5.9 for the rows (7.2).
+template <bool REFS>
 __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
   extern __shared__ uint32_t lds[];
   const int tid = threadIdx.x, B = a.B;
@@ -132,7 +186,11 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
   bool returns = own_count < 0, refused = false;
   for (int b = tid + PT; b < B; b += PT) returns |= a.count[b] < 0;
   if (a.reset) {
-    for (int i = tid; i < a.n_pages; i += PT) a.free[i] = a.n_pages - 1 - i;
+    for (int i = tid; i < a.n_pages; i += PT) {
+      a.free[i] = a.n_pages - 1 - i;
+      if constexpr (REFS) set_count(a.refs, i, 0);
+    }
+    if constexpr (REFS) settled_barrier();
   } else if (__syncthreads_or(returns)) {
     for (int b0 = 0; b0 < B; b0 += PT) {
       const int b = b0 + tid;
@@ -143,6 +201,14 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
     }
     if (tid == 0) first_page[B] = back[0];
     __syncthreads();  // first_page is whole
+    if constexpr (REFS) {
+      for (uint32_t i = tid; i < back[0]; i += PT) {
+        const int b = owner(first_page, B, i), page = a.table[(int64_t)b * a.max_pages + (i - first_page[b])];
+        if ((uint32_t)page < (uint32_t)a.n_pages) atomicSub(a.refs + page, 1);
+      }
+      n_free += push_unheld(a.table, a.refs, a.free, B, a.max_pages, a.n_pages, n_free, first_page, back[0],
+                            [&](int) { return true; }, part);
+    } else {
     const uint32_t given = min(back[0], (uint32_t)(a.n_pages - n_free));  // more only if a table holds a page twice
     for (uint32_t i = 4 * tid; i < given; i += 4 * PT) {
       int b[4];
@@ -152,6 +218,7 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
         if (i + u < given) a.free[n_free + i + u] = a.table[(int64_t)b[u] * a.max_pages + (i + u - first_page[b[u]])];
     }
     n_free += (int)given;
+    }
     __syncthreads();  // first_page is used anew, and the pages below are taken from the stack
   }
 
@@ -167,6 +234,13 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
         else {
           need = (uint32_t)max(0, pages_of(start + n, a.shift) - (int)held);
           count = (uint32_t)n;
+          if constexpr (REFS) {
+            for (int j = start >> a.shift; j < min((int)held, pages_of(start + n, a.shift)) && status == 0; ++j) {
+              const int page = a.table[(int64_t)b * a.max_pages + j];
+              if ((uint32_t)page < (uint32_t)a.n_pages && count_of(a.refs, page) > 1) status = CORA_ERR_STATE;
+            }
+            if (status != 0) need = count = 0;
+          }
         }
       }
     }
@@ -218,7 +292,11 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
       if (i + u < pages) page[u] = top ? top[-(int)(i + u)] : (int)(i + u);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (i + u < pages) a.table[(int64_t)b[u] * a.max_pages + have[b[u]] + (i + u - first_page[b[u]])] = page[u];
+      if (i + u < pages) {
+        a.table[(int64_t)b[u] * a.max_pages + have[b[u]] + (i + u - first_page[b[u]])] = page[u];
+        if constexpr (REFS)
+          if ((uint32_t)page[u] < (uint32_t)a.n_pages) set_count(a.refs, page[u], 1);
+      }
   }
   if (!a.rows_apart)
     for (uint32_t r = 4 * tid; r < (uint32_t)a.rows; r += 4 * PT) place_rows(a, first_row, r, first_page, have, top);
@@ -243,10 +321,166 @@ __global__ __launch_bounds__(256) void k_cache_rows(CachePlanArgs a) {
 hipError_t launch_cache_plan(CachePlanArgs a, hipStream_t s) {
   if (a.B > CACHE_MAX_BATCH) return hipErrorInvalidValue;
   a.rows_apart = a.rows > 8192;
-  hipLaunchKernelGGL(k_cache_plan, dim3(1), dim3(PT), (size_t)(3 * (a.B + 1)) * 4, s, a);
+  if (a.refs) hipLaunchKernelGGL(k_cache_plan<true>, dim3(1), dim3(PT), (size_t)(3 * (a.B + 1)) * 4, s, a);
+  else hipLaunchKernelGGL(k_cache_plan<false>, dim3(1), dim3(PT), (size_t)(3 * (a.B + 1)) * 4, s, a);
   if (hipError_t e = hipGetLastError()) return e;
   if (a.rows_apart) hipLaunchKernelGGL(k_cache_rows, dim3(((unsigned)a.rows + 1023) / 1024), dim3(256),
                                        (size_t)(a.B + 1) * 4, s, a);
+  return hipGetLastError();
+}
+
+// ---- requests that go on as their parents ------------------------------------------------------------------
+// With c children of request p: its full pages gain c - 1 holders, its last, partly filled one stays with
+// the first child and is let go of where there is none.  One workgroup counts children, changes the
+// counts, pushes what nobody holds, pops a page for each further child of a partly filled last page, and
+// writes the tables, all requests of some columns at a time (a request's row may be another's source).
+constexpr int RE = 8;  // table entries a thread holds between reading and writing
+
+__global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
+  extern __shared__ uint32_t lds[];
+  const int tid = threadIdx.x, B = a.B;
+  uint32_t* first = lds;                                   // exclusive prefix of the pages held, [B + 1]
+  int* parent = reinterpret_cast<int*>(lds + B + 1);       // -1: none
+  int* children = parent + B;
+  int* eldest = children + B;                              // a parent's lowest child
+  int* length = eldest + B;                                // before the call
+  int* fresh = length + B;                                 // page of the copy a request gets, or -1
+  __shared__ uint32_t part[2][PT / 64];
+  const int most = a.max_pages << a.shift;
+  const int n_free0 = min(max(a.n_free[0], 0), a.n_pages);
+  for (int b = tid; b < B; b += PT) {
+    const int p = a.parent[b];
+    const bool valid = p >= -1 && p < B;
+    parent[b] = valid ? p : b;
+    a.status[b] = valid ? 0 : CORA_ERR_INVALID_ARG;
+    length[b] = min(max(a.len[b], 0), most);
+    children[b] = 0;
+    eldest[b] = INT_MAX;
+    fresh[b] = -1;
+  }
+  __syncthreads();
+  for (int b = tid; b < B; b += PT)
+    if (parent[b] >= 0) {
+      atomicAdd(&children[parent[b]], 1);
+      atomicMin(&eldest[parent[b]], b);
+    }
+  uint32_t carry[2] = {0, 0};
+  int longest = 0;
+  for (int b0 = 0; b0 < B; b0 += PT) {
+    const int b = b0 + tid;
+    const int held = b < B ? pages_of(length[b], a.shift) : 0;
+    longest = max(longest, held);
+    uint32_t v[2] = {(uint32_t)held, 0};
+    block_scan(v, carry, part);
+    if (b < B) first[b] = v[0] - (uint32_t)held;
+  }
+  const uint32_t total = carry[0];
+  if (tid == 0) first[B] = total;
+  __syncthreads();
+
+  // the counts
+  bool drop = false;
+  for (uint32_t i = tid; i < total; i += PT) {
+    const int b = owner(first, B, i), at = (int)(i - first[b]);
+    const bool full = at < length[b] >> a.shift;
+    const int change = children[b] == 0 ? -1 : (full ? children[b] - 1 : 0);
+    drop |= children[b] == 0;
+    if (change == 0) continue;
+    const int page = a.table[(int64_t)b * a.max_pages + at];
+    if ((uint32_t)page < (uint32_t)a.n_pages) atomicAdd(a.refs + page, change);
+  }
+  int n_free = n_free0;
+  if (__syncthreads_or(drop))
+    n_free += push_unheld(a.table, a.refs, a.free, B, a.max_pages, a.n_pages, n_free, first, total,
+                          [&](int b) { return children[b] == 0; }, part);
+
+  // a page for each further child of a partly filled last page
+  uint32_t asked[2] = {0, 0};
+  for (int b0 = 0; b0 < B; b0 += PT) {
+    const int b = b0 + tid, p = b < B ? parent[b] : -1;
+    const bool wants = p >= 0 && eldest[p] != b && (length[p] & ((1 << a.shift) - 1)) != 0;
+    uint32_t v[2] = {wants ? 1u : 0u, 0};
+    block_scan(v, asked, part);
+    if (!wants) continue;
+    const int at = (int)v[0] - 1;
+    if (at >= n_free) {  // its share of the parent's full pages is let go of again
+      a.status[b] = CORA_ERR_OOM;
+      parent[b] = -1;
+      for (int j = 0; j < length[p] >> a.shift; ++j) {
+        const int page = a.table[(int64_t)p * a.max_pages + j];
+        if ((uint32_t)page < (uint32_t)a.n_pages) atomicSub(a.refs + page, 1);
+      }
+      continue;
+    }
+    const int src = a.table[(int64_t)p * a.max_pages + (length[p] >> a.shift)], dst = a.free[n_free - 1 - at];
+    fresh[b] = dst;
+    const bool known = (uint32_t)src < (uint32_t)a.n_pages && (uint32_t)dst < (uint32_t)a.n_pages;
+    if ((uint32_t)dst < (uint32_t)a.n_pages) set_count(a.refs, dst, 1);
+    int32_t* move = a.moves + 1 + 3 * at;
+    move[0] = src;
+    move[1] = dst;
+    move[2] = known ? ((length[p] & ((1 << a.shift) - 1)) + 31) / 32 : 0;
+  }
+  const int copies = min((int)asked[0], n_free);
+  if (tid == 0) {
+    a.moves[0] = copies;
+    a.n_free[0] = n_free - copies;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+  if ((tid & 63) == 0) part[0][tid >> 6] = (uint32_t)longest;
+  __syncthreads();
+  for (int w = 0; w < PT / 64; ++w) longest = max(longest, (int)part[0][w]);
+
+  // the tables
+  const int cols = max(1, min(longest, PT * RE / B)), n = B * cols;
+  for (int c0 = 0; c0 < longest; c0 += cols) {
+    int value[RE];
+#pragma unroll
+    for (int u = 0; u < RE; ++u) {
+      const int e = tid + u * PT, b = e / cols, col = c0 + e % cols;
+      const int p = e < n ? parent[b] : -1;
+      value[u] = INT_MIN;
+      if (p < 0 || (p == b && fresh[b] < 0) || col >= pages_of(length[p], a.shift)) continue;
+      value[u] = fresh[b] >= 0 && col == length[p] >> a.shift ? fresh[b] : a.table[(int64_t)p * a.max_pages + col];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < RE; ++u) {
+      const int e = tid + u * PT, b = e / cols, col = c0 + e % cols;
+      if (e < n && value[u] != INT_MIN) a.table[(int64_t)b * a.max_pages + col] = value[u];
+    }
+  }
+  for (int b = tid; b < B; b += PT) a.len[b] = parent[b] >= 0 ? length[parent[b]] : 0;
+}
+
+// The copies: 32 positions of one head, layer and of K or V at a time, contiguous in the page.
+__global__ __launch_bounds__(256) void k_cache_move(CacheReorderArgs a) {
+  const int per_page = (1 << a.shift) / 32, group = 32 * a.hd;  // elements of 32 positions
+  const int64_t page = (int64_t)group * per_page, units = (int64_t)a.moves[0] * a.n_layers * 2 * a.Hkv * per_page;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    int64_t r = u / per_page;
+    const int g = (int)(u - r * per_page);
+    const int h = (int)(r % a.Hkv);
+    r /= a.Hkv;
+    const int l = (int)(r % (2 * a.n_layers));
+    const int32_t* move = a.moves + 1 + 3 * (r / (2 * a.n_layers));
+    if (g >= move[2]) continue;
+    uint16_t* layer = (l & 1 ? a.v : a.k) + (int64_t)(l >> 1) * a.n_pages * a.Hkv * page;
+    const uint16_t* src = layer + ((int64_t)move[0] * a.Hkv + h) * page + (int64_t)g * group;
+    uint16_t* dst = layer + ((int64_t)move[1] * a.Hkv + h) * page + (int64_t)g * group;
+    for (int i = threadIdx.x * 8; i < group; i += 2048)
+      *reinterpret_cast<u32x4_t*>(dst + i) = *reinterpret_cast<const u32x4_t*>(src + i);
+  }
+}
+
+hipError_t launch_cache_reorder(const CacheReorderArgs& a, hipStream_t s) {
+  if (a.B > CACHE_MAX_BATCH) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_cache_reorder, dim3(1), dim3(PT), (size_t)(6 * a.B + 1) * 4, s, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (a.B == 1) return hipSuccess;  // a lone request has no second child
+  const int64_t units = (int64_t)(a.B - 1) * a.n_layers * 2 * a.Hkv * ((1 << a.shift) / 32);
+  hipLaunchKernelGGL(k_cache_move, dim3((unsigned)std::min<int64_t>(units, 2048)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -67,8 +67,18 @@ struct CachePlanArgs {
   int32_t *cu, *positions, *slots, *status;
   int B, max_pages, n_pages, shift, rows, reset;  // page size 1 << shift
   int rows_apart;                                 // set by the launcher
+  int32_t* refs;                                  // null: a page has one holder
 };
 hipError_t launch_cache_plan(CachePlanArgs a, hipStream_t s);
+struct CacheReorderArgs {
+  int32_t *table, *len, *free, *n_free, *refs;
+  const int32_t* parent;
+  int32_t *status, *moves;
+  int B, max_pages, n_pages, shift;
+  uint16_t *k, *v;
+  int n_layers, Hkv, hd;
+};
+hipError_t launch_cache_reorder(const CacheReorderArgs& a, hipStream_t s);
 // Rows [0, cu_end[0]) of x = [q | k | v], bf16 (xb) or the sum of `splits` fp32 slabs and the bias
 // (xf), row stride ld.  q may be null.
 struct CacheStoreArgs {

@@ -1053,8 +1053,27 @@ extern "C" cora_status cora_cache_plan(cora_pages* p, cora_chunk* c, int32_t res
   a.start = c->start; a.count = c->count;
   a.cu = c->cu; a.positions = c->positions; a.slots = c->slots; a.status = c->status;
   a.B = p->B; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.shift = page_shift(p->page_size);
-  a.rows = c->rows; a.reset = reset ? 1 : 0;
+  a.rows = c->rows; a.reset = reset ? 1 : 0; a.refs = p->refs;
   HIP_TRY(launch_cache_plan(a, S(hip_stream)));
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_cache_reorder(const cora_cache* cache, cora_pages* p, const int32_t* d_parent,
+                                          int32_t* d_status, int32_t* d_moves, void* hip_stream) try {
+  if (cora_status e = check_cache(cache, 0)) return e;
+  if (cora_status e = check_pages(p)) return e;
+  if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
+    return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
+  if (!p->refs) return fail(CORA_ERR_INVALID_ARG, "a reorder needs the pages' refs");
+  if (!d_parent || !d_status || !d_moves) return fail(CORA_ERR_INVALID_ARG, "null parent, status or moves");
+  CacheReorderArgs a{};
+  a.table = p->table; a.len = p->len; a.free = p->free; a.n_free = p->n_free; a.refs = p->refs;
+  a.parent = d_parent; a.status = d_status; a.moves = d_moves;
+  a.B = p->B; a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.shift = page_shift(p->page_size);
+  a.k = cache->k; a.v = cache->v; a.n_layers = cache->n_layers; a.Hkv = cache->n_kv_heads; a.hd = cache->head_dim;
+  HIP_TRY(launch_cache_reorder(a, S(hip_stream)));
   return CORA_OK;
 } catch (...) {
   return exception_status();
