@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "rows8.hpp"
+#include "tiles.hpp"
 
 namespace cora {
 
@@ -270,6 +271,138 @@ __global__ __launch_bounds__(WAVES * 64) void k_rows8_stream(Rows8ProductArgs g)
   }
 }
 
+// Tiles of many rows.  A workgroup of WM x WN wavefronts owns a tile, a wavefront TM x TN blocks of
+// 16 x 16.  Two stages of 128 columns in LDS, filled by loads that write LDS directly, hold operands and
+// scales as they lie in memory.  The MFMAs of a section work from registers; each fragment is reloaded with the
+// next section's as soon as its last MFMA is issued, half the section before it is needed: the first
+// TM / 2 rows with all columns, then the others, so that columns are free one by one in the second half.
+// The section's one barrier stands before the first reload: what it waits for (the next stage's loads, this
+// wavefront's reads of the stage that is overwritten from then on) is long done.
+template <int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArgs g, float* parts, int splits, int f32) {
+  constexpr int NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, GA = BM / 16, GB = BN / 16;
+  constexpr int STAGE = (BM + BN) * 132;                 // 128 columns and a dword of scales a row
+  constexpr int LPW = (GA + GB) * 2 / NW;                // loads of 1 KB a wavefront
+  static_assert((GA + GB) % NW == 0 && (BM + BN) % (NW * 64) == 0, "every wavefront loads alike");
+  constexpr int SPW = (BM + BN) / (NW * 64);             // loads of 64 scales a wavefront
+  static_assert(TM % 2 == 0, "two halves");
+  extern __shared__ __attribute__((aligned(1024))) char stages[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int li = xcd_remap(blockIdx.x, gridDim.x), n_tiles = gridDim.x / splits, split = li / n_tiles;
+  int tile_m, tile_n;
+  tile_of(li - split * n_tiles, (g.M + BM - 1) / BM, n_tiles, tile_m, tile_n);
+  const int nk_all = r8_blocks(g.K), nq = r8_quads(g.K);
+  const int k0 = (int)((int64_t)nk_all * split / splits), nk = (int)((int64_t)nk_all * (split + 1) / splits) - k0;
+  const int ga0 = tile_m * GA, gb0 = tile_n * GB;        // first row groups
+  const int a_last = (g.M + 15) / 16 - 1 - ga0, b_last = (g.N + 15) / 16 - 1 - gb0;
+
+  // this wavefront's loads: LPW / 2 row groups of A or W, clamped to the last one, and 64 scales SPW times
+  u32x4_t rs[LPW / 2], ss[SPW];
+  int vo[LPW / 2], vs[SPW];
+  const u32x4_t a_rs = buffer_rsrc(g.a + (int64_t)ga0 * nk_all * R8_BLOCK, (int64_t)(a_last + 1) * nk_all * R8_BLOCK);
+  const u32x4_t b_rs = buffer_rsrc(g.w + (int64_t)gb0 * nk_all * R8_BLOCK, (int64_t)(b_last + 1) * nk_all * R8_BLOCK);
+  const u32x4_t as_rs = buffer_rsrc(g.a_scale + (int64_t)ga0 * nq * 64, (int64_t)(a_last + 1) * nq * 64);
+  const u32x4_t bs_rs = buffer_rsrc(g.w_scale + (int64_t)gb0 * nq * 64, (int64_t)(b_last + 1) * nq * 64);
+#pragma unroll
+  for (int t = 0; t < LPW / 2; ++t) {
+    const int grp = wave * (LPW / 2) + t;
+    const bool is_a = grp < GA;
+    rs[t] = is_a ? a_rs : b_rs;
+    vo[t] = (is_a ? min(grp, a_last) : min(grp - GA, b_last)) * nk_all * R8_BLOCK + lane * 16;
+  }
+#pragma unroll
+  for (int t = 0; t < SPW; ++t) {
+    const int row0 = (wave * SPW + t) * 64;
+    const bool is_a = row0 < BM;
+    const int row = (is_a ? row0 : row0 - BM) + lane;
+    ss[t] = is_a ? as_rs : bs_rs;
+    vs[t] = min(row >> 4, is_a ? a_last : b_last) * nq * 64 + (row & 15) * 4;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)stages;
+  auto issue = [&](int kt, uint32_t st, int t) {  // load t of slice kt into the stage at st
+    const int k = k0 + kt;
+    if (t < LPW) load_lds(lds0 + st + (wave * LPW + t) * 1024, vo[t / 2], rs[t / 2], k * R8_BLOCK + (t & 1) * 1024);
+    else load_lds_dword(lds0 + st + (BM + BN) * 128 + (wave * SPW + t - LPW) * 256, vs[t - LPW < 0 ? 0 : t - LPW], ss[t - LPW < 0 ? 0 : t - LPW], (k >> 2) * 64);
+  };
+
+  f32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  i32x8_t fa[TM], fb[TN];
+  uint32_t sa[TM], sb[TN];
+  const int a_at = wm * TM * R8_BLOCK + lane * 16, b_at = (GA + wn * TN) * R8_BLOCK + lane * 16;
+  const int as_at = (BM + BN) * 128 + (wm * TM * 16 + (lane & 15)) * 4, bs_at = (BM + BN) * 128 + (BM + wn * TN * 16 + (lane & 15)) * 4;
+  auto frag = [&](int at) {
+    return both(*reinterpret_cast<const u32x4_t*>(stages + at), *reinterpret_cast<const u32x4_t*>(stages + at + 1024));
+  };
+  auto read_a = [&](int st, int by, int i) {
+    fa[i] = frag(st + a_at + i * R8_BLOCK);
+    sa[i] = *reinterpret_cast<const uint8_t*>(stages + st + as_at + by + i * 64);
+  };
+  auto read_b = [&](int st, int by, int j) {
+    fb[j] = frag(st + b_at + j * R8_BLOCK);
+    sb[j] = *reinterpret_cast<const uint8_t*>(stages + st + bs_at + by + j * 64);
+  };
+  constexpr int NM = TM * TN, HALF = TM / 2, BAR = NM / 2 - 2 < 0 ? 0 : NM / 2 - 2, ALL = LPW + SPW;
+  auto section = [&](auto more_c, int kt, int st, int nx) {
+    constexpr bool MORE = decltype(more_c)::value;
+    const int by = (k0 + kt + 1) & 3;
+#pragma unroll
+    for (int q = 0; q < NM; ++q) {
+      const int half = q / (HALF * TN), j = q % (HALF * TN) / HALF, i = half * HALF + q % HALF;
+      if (MORE && q == BAR) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      acc[i][j] = mfma<0>(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
+      if constexpr (MORE) {
+        if (j == TN - 1) read_a(nx, by, i);
+        if (half == 1 && i == TM - 1) read_b(nx, by, j);
+#pragma unroll
+        for (int t = 0; t < ALL; ++t)
+          if (BAR + t * (NM - BAR) / ALL == q) issue(min(kt + 2, nk - 1), (uint32_t)st, t);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (nk > 0) {
+#pragma unroll
+    for (int t = 0; t < ALL; ++t) issue(0, 0, t);
+#pragma unroll
+    for (int t = 0; t < ALL; ++t) issue(min(1, nk - 1), STAGE, t);
+    wait_vm<ALL>();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) read_a(0, k0 & 3, i);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) read_b(0, k0 & 3, j);
+    int st = 0;
+    for (int kt = 0; kt + 1 < nk; ++kt) {
+      section(std::true_type{}, kt, st, STAGE - st);
+      st = STAGE - st;
+    }
+    section(std::false_type{}, nk - 1, 0, 0);
+    wait_vm<0>();
+  }
+
+  // a lane holds row lane % 16 and columns 4 (lane / 16) .. + 3 of each block
+  const int row0 = tile_m * BM + wm * TM * 16 + (lane & 15), col0 = tile_n * BN + wn * TN * 16 + 4 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = row0 + i * 16;
+    if (row >= g.M) continue;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int col = col0 + j * 16;
+      if (col >= g.N) continue;
+      store4<false>(g, row, col, acc[i][j]);
+    }
+  }
+}
+
 Rows8Plan rows8_plan(int, int, int, int) { return Rows8Plan{0}; }
 
 template <int MB, int NB, int WAVES>
@@ -281,7 +414,18 @@ static hipError_t run_stream(const Rows8ProductArgs& a, bool f32, hipStream_t s)
   return hipGetLastError();
 }
 
+template <int WM, int WN, int TM, int TN>
+static hipError_t run_tiles(const Rows8ProductArgs& a, hipStream_t s) {
+  constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
+  constexpr unsigned LDS = 2 * (BM + BN) * 132;
+  static_assert(LDS <= 160 * 1024, "LDS of a CU");
+  const int grid = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
+  hipLaunchKernelGGL((k_rows8_tiles<WM, WN, TM, TN>), dim3(grid), dim3(WM * WN * 64), LDS, s, a, nullptr, 1, 0);
+  return hipGetLastError();
+}
+
 hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan&, bool f32, float*, hipStream_t s) {
+  if (!f32 && a.M > 64) return run_tiles<4, 2, 4, 8>(a, s);
   if (a.M <= 16) return run_stream<1, 2, 4>(a, f32, s);
   if (a.M <= 32) return run_stream<2, 2, 4>(a, f32, s);
   return run_stream<4, 2, 4>(a, f32, s);
