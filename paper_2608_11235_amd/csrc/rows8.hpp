@@ -33,10 +33,20 @@ struct Rows8ProductArgs {
   const float* bias;
   void* out; int64_t ld;
 };
+// How a product runs, made from its sizes alone.
 struct Rows8Plan {
+  bool few;              // activations kept in registers (k_rows8_few), or tiles
+  int cfg;               // tiles: their config
+  int mb, nb, sq, kw, grid;  // few: groups of activation and weight rows and quads of blocks a wavefront, wavefronts along the columns
+  int splits;            // workgroups along the columns, whose sums a second kernel adds
   size_t ws_floats;
 };
-Rows8Plan rows8_plan(int M, int N, int K, int num_cus);
-hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, float* ws, hipStream_t s);
+struct Rows8Few { int kw; };
+// wide: results in fp32 with sums of 32 bits (else those of the 8-bit instruction)
+Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus);
+Rows8Plan rows8_plan_few(int M, int N, int K, int nb, int sq, int ranges, bool wide, int num_cus);
+int rows8_few_rows(bool wide);  // of a launch
+Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus);
+hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s);
 
 }  // namespace cora

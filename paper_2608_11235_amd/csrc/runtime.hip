@@ -1329,7 +1329,8 @@ static cora_status check_product_sizes(int32_t M, int32_t N, int32_t cols) {
 extern "C" cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, size_t* bytes) try {
   if (!bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
   if (cora_status e = check_product_sizes(M, N, cols)) return e;
-  *bytes = 4 * rows8_plan(M, N, cols, current_cus()).ws_floats;
+  const int cus = current_cus();  // enough for either type of result
+  *bytes = 4 * std::max(rows8_plan(M, N, cols, false, cus).ws_floats, rows8_plan(M, N, cols, true, cus).ws_floats);
   return CORA_OK;
 } catch (...) {
   return exception_status();
@@ -1347,11 +1348,11 @@ extern "C" cora_status cora_rows_product(const cora_rows8* a, const cora_rows8* 
   if (!d_out || ld < N || (reinterpret_cast<uintptr_t>(d_out) & (out_f32 ? 3 : 1)) != 0 ||
       (reinterpret_cast<uintptr_t>(d_bias) & 3) != 0)
     return fail(CORA_ERR_INVALID_ARG, "out must be given, ld >= N, out and bias aligned to their elements");
-  const Rows8Plan pl = rows8_plan(M, N, a->cols, current_cus());
+  const Rows8Plan pl = rows8_plan(M, N, a->cols, out_f32 != 0, current_cus());
   if (pl.ws_floats && (!workspace || !aligned16(workspace) || workspace_bytes < pl.ws_floats * 4))
     return fail(CORA_ERR_INVALID_ARG, "workspace missing, misaligned or smaller than cora_rows_product_workspace says");
   const Rows8ProductArgs g{a->data, a->scale, w->data, w->scale, M, N, a->cols, d_bias, d_out, ld};
-  HIP_TRY(launch_rows8_product(g, pl, out_f32 != 0, static_cast<float*>(workspace), S(hip_stream)));
+  HIP_TRY(launch_rows8_product(g, pl, out_f32 != 0, out_f32 != 0, static_cast<float*>(workspace), S(hip_stream)));
   return CORA_OK;
 } catch (...) {
   return exception_status();
