@@ -144,14 +144,16 @@ __device__ __forceinline__ bf16x8_t widened(uint32_t lo, uint32_t hi) {
 }
 // The same by the bf16 instruction, whose sums keep 32 bits: sum first, then the scales.  ws: the scales
 // of the lane's four weight rows.
-template <int U>
-__device__ __forceinline__ f32x4_t mfma_wide(i32x8_t w, i32x8_t a, f32x4_t acc, u32x4_t ws, uint32_t as) {
+struct Wide { bf16x8_t k[4]; };
+__device__ __forceinline__ Wide widened(i32x8_t x) {
+  return Wide{{widened(x[0], x[1]), widened(x[2], x[3]), widened(x[4], x[5]), widened(x[6], x[7])}};
+}
+__device__ __forceinline__ f32x4_t mfma_wide(const Wide& w, const Wide& a, f32x4_t acc, u32x4_t ws, uint32_t as, int byte) {
   f32x4_t p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(w[2 * t], w[2 * t + 1]), widened(a[2 * t], a[2 * t + 1]), p, 0, 0, 0);
+  for (int t = 0; t < 4; ++t) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.k[t], a.k[t], p, 0, 0, 0);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] += ldexpf(p[e], (int)(ws[e] >> 8 * U & 255) + (int)(as >> 8 * U & 255) - 254);
+  for (int e = 0; e < 4; ++e) acc[e] += ldexpf(p[e], (int)(ws[e] >> 8 * byte & 255) + (int)(as >> 8 * byte & 255) - 254);
   return acc;
 }
 
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
       for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          if constexpr (WIDE) acc[m][n] = mfma_wide<U & 3>(w[n][U & 3], a[m][U], acc[m][n], ws[n][U / 4], as[m][U / 4]);
+          if constexpr (WIDE) acc[m][n] = mfma_wide(widened(w[n][U & 3]), widened(a[m][U]), acc[m][n], ws[n][U / 4], as[m][U / 4], U & 3);
           else acc[m][n] = mfma<U & 3>(w[n][U & 3], a[m][U], acc[m][n], ws[n][U / 4], as[m][U / 4]);
         }
       __builtin_amdgcn_sched_barrier(0);
@@ -323,7 +325,9 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
 //
 // A tile's results pass through LDS of the wavefront's own and leave as runs of CB x 32 bytes, 16 a lane, behind the
 // next tile's first loads (4096 x 37888 bf16 written alone in runs of 32 bytes 81 us, of 64 58 us, of 256 56 us).
-template <int WM, int WN, int TM, int TN, int ST, int CB, int OUT>
+// WIDE (sums of 32 bits): a section's fragments are widened to bf16 first, the activations all, a group of weight
+// rows at a time; they are free at once, and the barrier stands between.
+template <int WM, int WN, int TM, int TN, int ST, int CB, int OUT, bool WIDE>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArgs g, int splits) {
   constexpr int NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, GA = BM / 16, GB = BN / 16;
   constexpr int ROWS = BM + BN, STAGE = ROWS * 132;       // 128 columns and a dword of scales a row
@@ -392,28 +396,64 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   // ---- the products
   f32x4_t acc[TM][TN];
   i32x8_t fa[TM], fb[TN];
-  uint32_t sa[TM], sb[TN];
+  std::conditional_t<WIDE, u32x4_t, uint32_t> sb[TN];  // WIDE: the dwords of the lane's four weight rows
+  uint32_t sa[TM];
   const int a_at = wm * TM * R8_BLOCK + lane * 16, b_at = (GA + wn * TN) * R8_BLOCK + lane * 16;
-  const int as_at = ROWS * 128 + (wm * TM * 16 + r16) * 4, bs_at = ROWS * 128 + (BM + wn * TN * 16 + r16) * 4;
+  const int as_at = ROWS * 128 + (wm * TM * 16 + r16) * 4, bs_at = ROWS * 128 + (BM + wn * TN * 16 + (WIDE ? 4 * g4 : r16)) * 4;
   auto frag = [&](int at) {
     return both(*reinterpret_cast<const u32x4_t*>(stages + at), *reinterpret_cast<const u32x4_t*>(stages + at + 1024));
   };
   auto read_a = [&](int st, int by, int i) {
     fa[i] = frag(st + a_at + i * R8_BLOCK);
-    sa[i] = *reinterpret_cast<const uint8_t*>(stages + st + as_at + by + i * 64);
+    if constexpr (WIDE) sa[i] = *reinterpret_cast<const uint32_t*>(stages + st + as_at + i * 64);
+    else sa[i] = *reinterpret_cast<const uint8_t*>(stages + st + as_at + by + i * 64);
   };
   auto read_b = [&](int st, int by, int j) {
     fb[j] = frag(st + b_at + j * R8_BLOCK);
-    sb[j] = *reinterpret_cast<const uint8_t*>(stages + st + bs_at + by + j * 64);
+    if constexpr (WIDE) sb[j] = *reinterpret_cast<const u32x4_t*>(stages + st + bs_at + j * 64);
+    else sb[j] = *reinterpret_cast<const uint8_t*>(stages + st + bs_at + by + j * 64);
   };
   constexpr int NM = TM * TN, HALF = TM / 2, BAR = NM / 2 >= 2 ? NM / 2 - 2 : 0;
   constexpr int RUNS = 16 * CB * 2 / 64, STORES = OUT == OUT_BF16 ? TM * (TN / CB) * RUNS : 0;
   int st = 0;           // stage of the section at hand
+  int this_by = 0;      // WIDE: byte of its scales
   bool late = false;    // a tile's stores, all STORES of them, were issued since the loads that a barrier waits for
   // FIRST: of a tile; by: byte of the next section's scales
   auto section = [&](auto first_c, int by) {
     constexpr bool FIRST = decltype(first_c)::value;
     const int nx = st + STAGE == ST * STAGE ? 0 : st + STAGE;
+    if constexpr (WIDE) {
+      Wide a[TM];
+      uint32_t as[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        a[i] = widened(fa[i]);
+        as[i] = sa[i];
+        if constexpr (FIRST) {
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      wait_vm<(ST - 2) * ALL>();
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) read_a(nx, by, i);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const Wide w = widened(fb[j]);
+        const u32x4_t ws = sb[j];
+        read_b(nx, by, j);
+#pragma unroll
+        for (int t = 0; t < ALL; ++t)
+          if (t * TN / ALL == j) issue((uint32_t)st, t);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j] = mfma_wide(w, a[i], acc[i][j], ws, as[i], this_by);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      this_by = by;
+    } else {
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
       const int half = q / (HALF * TN), j = q % (HALF * TN) / HALF, i = half * HALF + q % HALF;
@@ -430,6 +470,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
       for (int t = 0; t < ALL; ++t)
         if (BAR + t * (NM - BAR) / ALL == q) issue((uint32_t)st, t);
       __builtin_amdgcn_sched_barrier(0);
+    }
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -449,6 +490,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   __syncthreads();
   int k0, k1;
   k_range(first, k0, k1);
+  this_by = k0 & 3;
 #pragma unroll
   for (int i = 0; i < TM; ++i) read_a(0, k0 & 3, i);
 #pragma unroll
@@ -555,9 +597,13 @@ static R8Shape r8_shape(int cfg) {
 // latency a section and the chip's throughput, plus what a tile takes besides; the stream of weights, a fifth of which
 // goes beside it; the sums of split columns.  Fitted to all configs and splits of 209 shapes (80 to 4096 rows, 688 to
 // 37888 weight rows, 1000 to 12288 columns; 12 % off in the mean).  What it picks is on average 1 %, at most 15 % slower
-// than the fastest of these.
-static double tiles_us(int M, int N, int K, int cfg, int splits, int num_cus) {
-  const R8Shape sh = r8_shape(cfg);
+// than the fastest of these.  Sections of 32-bit sums take 2.15 times as long.
+static double tiles_us(int M, int N, int K, int cfg, int splits, bool wide, int num_cus) {
+  R8Shape sh = r8_shape(cfg);
+  if (wide) {
+    sh.section_us *= 2.15;
+    sh.cu_us *= 2.15;
+  }
   const double sections = (double)r8_blocks(K) / splits;
   const int64_t items = (int64_t)((M + sh.bm - 1) / sh.bm) * ((N + sh.bn - 1) / sh.bn) * splits, slots = (int64_t)num_cus * sh.per_cu;
   auto round_us = [&](int64_t n) {
@@ -593,7 +639,7 @@ Rows8Plan rows8_plan_few(int M, int N, int K, int nb, int sq, int ranges, bool w
   if (p.kw > 8) p.splits = 0;  // no such plan
   const int64_t sets = (r8_groups(N) + nb - 1) / nb, wgs = (sets * p.kw + 7) / 8;
   p.grid = (int)std::min<int64_t>(wgs, std::max(1, num_cus / ranges));
-  p.ws_floats = ranges > 1 ? (size_t)ranges * std::min(M, rows8_few_rows(wide)) * ((N + 3) / 4 * 4) : 0;
+  p.ws_floats = ranges > 1 ? (size_t)ranges * M * ((N + 3) / 4 * 4) : 0;
   return p;
 }
 Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus) {
@@ -611,7 +657,7 @@ Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus
 constexpr int64_t R8_MOST_PARTS = 1 << 26;
 
 Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
-  if (M <= rows8_few_rows(wide) || wide) {
+  if (M <= rows8_few_rows(wide)) {
     // as many columns as a wavefront's registers hold, then more workgroups along them; two groups of weight
     // rows where there are enough for all CUs (32 x 24576 x 4096 19.4 us, with one 19.9)
     const int nq = r8_quads(K), mb = few_groups(M, wide), most = mb == 4 || (wide && mb == 2) ? 1 : (wide || mb == 2 ? 2 : 3);
@@ -628,10 +674,11 @@ Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
   for (int splits = 1; splits <= 8; splits *= 2) {
     if (splits > 1 && (r8_blocks(K) < 4 * splits || (int64_t)splits * M * ((N + 3) / 4 * 4) > R8_MOST_PARTS)) continue;
     for (int c = 0; c < R8_CONFIGS; ++c) {
+      if (wide && c != 3 && c != 5) continue;
       const R8Shape sh = r8_shape(c);
       // the smallest tiles read too much from L2 for more of them than CUs (with them the picks are 2.4 % slower in the mean)
-      if (c == 5 && (int64_t)((M + sh.bm - 1) / sh.bm) * ((N + sh.bn - 1) / sh.bn) * splits > num_cus) continue;
-      const double us = tiles_us(M, N, K, c, splits, num_cus);
+      if (c == 5 && !wide && (int64_t)((M + sh.bm - 1) / sh.bm) * ((N + sh.bn - 1) / sh.bn) * splits > num_cus) continue;
+      const double us = tiles_us(M, N, K, c, splits, wide, num_cus);
       if (best_us < 0 || us < best_us) { best_cfg = c; best_splits = splits; best_us = us; }
     }
   }
@@ -661,24 +708,27 @@ static hipError_t run_few(const Rows8ProductArgs& a, const Rows8Plan& p, hipStre
 #undef X
   return hipErrorInvalidValue;
 }
-template <int OUT>
-static hipError_t run_tiles(const Rows8ProductArgs& a, const Rows8Plan& p, hipStream_t s) {
-  switch (p.cfg) {
-#define X(C, WM, WN, TM, TN, ST, CB, PER, ...)                                                                       \
-  case C: {                                                                                                          \
-    constexpr unsigned LDS = ST * (WM * TM + WN * TN) * 16 * 132 + WM * WN * 16 * (CB * 32 + 16);                    \
-    static_assert(LDS * PER <= 160 * 1024, "LDS of a CU");                                                           \
-    hipLaunchKernelGGL((k_rows8_tiles<WM, WN, TM, TN, ST, CB, OUT>), dim3(p.grid), dim3(WM * WN * 64), LDS, s, a, p.splits); \
-    return hipGetLastError();                                                                                        \
-  }
-    R8_TILES(X)
-#undef X
-  }
-  return hipErrorInvalidValue;
-}
+// those of 32-bit sums, which need more registers
+#define R8_TILES_WIDE(X)     \
+  X(3, 2, 2, 4, 4, 2, 4, 2)  \
+  X(5, 2, 2, 2, 2, 4, 2, 2)
 
-static void* at_row(void* out, int64_t row, int64_t ld, bool f32) {
-  return static_cast<char*>(out) + row * ld * (f32 ? 4 : 2);
+template <int OUT, bool WIDE>
+static hipError_t run_tiles(const Rows8ProductArgs& a, const Rows8Plan& p, hipStream_t s) {
+#define X(C, WM, WN, TM, TN, ST, CB, PER, ...)                                                                           \
+  if (p.cfg == C) {                                                                                                      \
+    constexpr unsigned LDS = ST * (WM * TM + WN * TN) * 16 * 132 + WM * WN * 16 * (CB * 32 + 16);                        \
+    static_assert(LDS * PER <= 160 * 1024, "LDS of a CU");                                                               \
+    hipLaunchKernelGGL((k_rows8_tiles<WM, WN, TM, TN, ST, CB, OUT, WIDE>), dim3(p.grid), dim3(WM * WN * 64), LDS, s, a, p.splits); \
+    return hipGetLastError();                                                                                            \
+  }
+  if constexpr (WIDE) {
+    R8_TILES_WIDE(X)
+  } else {
+    R8_TILES(X)
+  }
+#undef X
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_rows8_product(const Rows8ProductArgs& in, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s) {
@@ -689,27 +739,10 @@ hipError_t launch_rows8_product(const Rows8ProductArgs& in, const Rows8Plan& p, 
     a.bias = nullptr;
   }
   const bool out_f32 = f32 || p.splits > 1;
-  hipError_t e = hipSuccess;
-  if (p.few) {
-    // more rows than that (results of 32-bit sums): as many at a time
-    const int step = rows8_few_rows(wide);
-    for (int m = 0; m < in.M && e == hipSuccess; m += step) {
-      Rows8ProductArgs b = a;
-      b.M = std::min(step, in.M - m);
-      b.a += (int64_t)(m / 16) * r8_blocks(a.K) * R8_BLOCK;
-      b.a_scale += (int64_t)(m / 16) * r8_quads(a.K) * 64;
-      if (p.splits == 1) b.out = at_row(a.out, m, a.ld, f32);
-      e = wide ? run_few<OUT_F32, true>(b, p, s) : (out_f32 ? run_few<OUT_F32, false>(b, p, s) : run_few<OUT_BF16, false>(b, p, s));
-      if (e == hipSuccess && p.splits > 1) {
-        Rows8ProductArgs o = in;
-        o.M = b.M;
-        o.out = at_row(in.out, m, in.ld, f32);
-        e = fold(o, static_cast<const float*>(b.out), p.splits, (int)a.ld, f32, s);
-      }
-    }
-    return e;
-  }
-  e = out_f32 ? run_tiles<OUT_F32>(a, p, s) : run_tiles<OUT_BF16>(a, p, s);
+  if (p.few && in.M > rows8_few_rows(wide)) return hipErrorInvalidValue;
+  hipError_t e;
+  if (p.few) e = wide ? run_few<OUT_F32, true>(a, p, s) : (out_f32 ? run_few<OUT_F32, false>(a, p, s) : run_few<OUT_BF16, false>(a, p, s));
+  else e = wide ? run_tiles<OUT_F32, true>(a, p, s) : (out_f32 ? run_tiles<OUT_F32, false>(a, p, s) : run_tiles<OUT_BF16, false>(a, p, s));
   if (e == hipSuccess && p.splits > 1) e = fold(in, ws, p.splits, (int)a.ld, f32, s);
   return e;
 }
