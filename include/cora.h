@@ -458,7 +458,8 @@ cora_status cora_quantize_rows(const void *d_x, int32_t x_f32, int64_t ld, const
  * aligned (NULL when that is 0): used from this call's start to its end on the stream, contents not
  * kept; calls that may overlap and captured graphs that may run at once need one each.  cols = 0 is
  * refused; M = 0 or N = 0 does nothing.  Asynchronous. */
-cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, size_t *bytes);
+cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, int32_t out_f32,
+                                        size_t *bytes);
 cora_status cora_rows_product(const cora_rows8 *a, const cora_rows8 *w, const float *d_bias,
                                void *d_out, int32_t out_f32, int64_t ld, void *workspace,
                                size_t workspace_bytes, void *hip_stream);

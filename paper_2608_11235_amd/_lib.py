@@ -98,7 +98,7 @@ EXPORTS = {
                                 c_vp, c_sz, c_vp]),
     "cora_rows_bytes": (c_i32, [c_i32, c_i32, _P(c_sz), _P(c_sz)]),
     "cora_quantize_rows": (c_i32, [c_vp, c_i32, c_i64, _P(Rows8), c_vp]),
-    "cora_rows_product_workspace": (c_i32, [c_i32, c_i32, c_i32, _P(c_sz)]),
+    "cora_rows_product_workspace": (c_i32, [c_i32, c_i32, c_i32, c_i32, _P(c_sz)]),
     "cora_rows_product": (c_i32, [_P(Rows8), _P(Rows8), c_vp, c_vp, c_i32, c_i64, c_vp, c_sz, c_vp]),
     "cora_model_copy_tensor": (c_i32, [c_vp, c_i32, c_vp, c_sz]),
     "cora_model_set_timing": (c_i32, [c_vp, c_i32]),

@@ -455,12 +455,18 @@ def cache_reorder(cache: KVCache, parent, status=None, moves=None, stream=None):
     if cache._refs is None:
         raise ValueError("cache: made without shared=True")
     B = cache._batch
-    if status is None:
-        status = _empty(B, torch.int32, cache._k.device, stream)
-    if moves is None:
-        moves = _empty(1 + 3 * B, torch.int32, cache._k.device, stream)
-    _call(device, "cora_cache_reorder", cache._cache, cache._pages, _checked(parent, "parent", _I32, B, device),
-          _checked(status, "status", _I32, B, device), _checked(moves, "moves", _I32, 1 + 3 * B, device), stream=stream)
+    if status is None and moves is None:  # one tensor for both
+        both = _empty(1 + 4 * B, torch.int32, cache._k.device, stream)
+        status, at = both[:B], both.data_ptr()
+        outs = at, at + 4 * B
+    else:
+        if status is None:
+            status = _empty(B, torch.int32, cache._k.device, stream)
+        if moves is None:
+            moves = _empty(1 + 3 * B, torch.int32, cache._k.device, stream)
+        outs = _checked(status, "status", _I32, B, device), _checked(moves, "moves", _I32, 1 + 3 * B, device)
+    _call(device, "cora_cache_reorder", cache._cache, cache._pages, _checked(parent, "parent", _I32, B, device), *outs,
+          stream=stream)
     return status
 
 
@@ -572,12 +578,19 @@ def vocab_beam(logits, beams, mask_id, score, width=None, done=None, done_token=
     B, W = R // beams, beams if width is None else width
     if W < 1:
         raise ValueError(f"width: {W}, at least one is needed")
-    if token is None:
-        token = _empty((B, W), torch.int32, logits.device, stream)
-    if parent is None:
-        parent = _empty((B, W), torch.int32, logits.device, stream)
-    if next_score is None:
-        next_score = _empty((B, W), torch.float32, logits.device, stream)
+    if token is None and parent is None and next_score is None:  # one tensor for the three
+        token, parent, next_score = _empty((3, B, W), torch.int32, logits.device, stream).unbind(0)
+        next_score = next_score.view(torch.float32)
+        outs = token.data_ptr(), parent.data_ptr(), next_score.data_ptr()
+    else:
+        if token is None:
+            token = _empty((B, W), torch.int32, logits.device, stream)
+        if parent is None:
+            parent = _empty((B, W), torch.int32, logits.device, stream)
+        if next_score is None:
+            next_score = _empty((B, W), torch.float32, logits.device, stream)
+        outs = (_checked(token, "token", _I32, B * W, device), _checked(parent, "parent", _I32, B * W, device),
+                _checked(next_score, "next_score", _F32, B * W, device))
     if workspace is None:
         key = (B, beams, V, W, device)
         n = _beam_workspaces.get(key)
@@ -586,17 +599,17 @@ def vocab_beam(logits, beams, mask_id, score, width=None, done=None, done_token=
                 _beam_workspaces.clear()
             n = _beam_workspaces[key] = vocab_beam_workspace(B, beams, V, W, device)
         workspace = _empty(n, torch.uint8, logits.device, stream)
+        at = workspace.data_ptr()
+    else:
+        at, n = _checked(workspace, "workspace", _U8, 0, device), workspace.numel()
     _call(device, "cora_vocab_beam", logits.data_ptr(), B, beams, V, ld, mask_id,
           _checked(score, "score", _F32, R, device),
-          None if done is None else _checked(done, "done", _FLAGS, R, device), done_token, W,
-          _checked(token, "token", _I32, B * W, device), _checked(parent, "parent", _I32, B * W, device),
-          _checked(next_score, "next_score", _F32, B * W, device),
-          _checked(workspace, "workspace", _U8, 0, device), workspace.numel(), stream=stream)
+          None if done is None else _checked(done, "done", _FLAGS, R, device), done_token, W, *outs, at, n, stream=stream)
     return token, parent, next_score
 
 
 # ---- 8-bit rows and their products ----------------------------------------------------------------
-@_fixed("data", "scale", "rows", "cols")
+@_fixed("rows", "cols")
 class Rows8:
     """A matrix [rows, cols] in 8-bit floating point, each 128 columns of a row with a power of two as
     their scale, in the order of the products' operands (cora_rows8).  Zeros at first.  `data` and `scale`
@@ -605,28 +618,37 @@ class Rows8:
     def __init__(self, rows, cols, device="cuda"):
         data, scale = ctypes.c_size_t(0), ctypes.c_size_t(0)
         check(_lib.load().cora_rows_bytes(rows, cols, ctypes.byref(data), ctypes.byref(scale)), "cora_rows_bytes")
-        self._hold(rows, cols, torch.zeros(data.value, dtype=torch.uint8, device=device),
-                   torch.full((scale.value,), 127, dtype=torch.uint8, device=device))
+        self._hold(rows, cols, data.value, torch.zeros(data.value + scale.value, dtype=torch.uint8, device=device))
+        self.scale.fill_(127)
 
-    def _hold(self, rows, cols, data, scale):
-        self._rows, self._cols, self._data, self._scale = rows, cols, data, scale
-        self._device = data.get_device()
-        self._c = ctypes.byref(_lib.Rows8(data.data_ptr(), scale.data_ptr(), rows, cols))
+    def _hold(self, rows, cols, n, buffer):
+        # one buffer, data in front; its halves are looked at by few programs and cost a call more than they do here
+        self._rows, self._cols, self._n, self._buffer = rows, cols, n, buffer
+        self._device = buffer.get_device()
+        at = buffer.data_ptr()
+        self._c = ctypes.byref(_lib.Rows8(at, at + n, rows, cols))
         return self
 
     @classmethod
     def _empty(cls, rows, cols, device, stream):
         """For a call that writes all of it."""
         groups = (rows + 15) // 16
-        return cls.__new__(cls)._hold(
-            rows, cols, _empty(groups * ((cols + 127) // 128) * 2048, torch.uint8, device, stream),
-            _empty(groups * ((cols + 511) // 512) * 64, torch.uint8, device, stream))
+        n = groups * ((cols + 127) // 128) * 2048
+        return cls.__new__(cls)._hold(rows, cols, n, _empty(n + groups * ((cols + 511) // 512) * 64, torch.uint8, device, stream))
+
+    @property
+    def data(self):
+        return self._buffer[:self._n]
+
+    @property
+    def scale(self):
+        return self._buffer[self._n:]
 
     def values(self):
         """The numbers that the rows stand for, float32 [rows, cols]."""
         groups, blocks = -(-self._rows // 16), -(-self._cols // 128)
-        q = self._data.view(torch.float8_e4m3fn).double().view(groups, blocks, 8, 16, 16)
-        s = self._scale.view(groups, -1, 16, 4).transpose(2, 3).reshape(groups, -1, 1, 16, 1)[:, :blocks]
+        q = self.data.view(torch.float8_e4m3fn).double().view(groups, blocks, 8, 16, 16)
+        s = self.scale.view(groups, -1, 16, 4).transpose(2, 3).reshape(groups, -1, 1, 16, 1)[:, :blocks]
         x = torch.ldexp(q, s.int() - 127).float().permute(0, 3, 1, 2, 4)  # in 64 bits: 2^-127 is no normal float32
         return x.reshape(groups * 16, blocks * 128)[:self._rows, :self._cols].contiguous()
 
@@ -649,14 +671,14 @@ def quantize_rows(x, out=None, stream=None):
 _product_workspaces = {}  # bytes that rows8_product needs, by its sizes
 
 
-def rows8_product_workspace(a: Rows8, w: Rows8):
-    """Bytes of workspace that rows8_product needs for these sizes."""
+def rows8_product_workspace(a: Rows8, w: Rows8, dtype=torch.bfloat16):
+    """Bytes of workspace that rows8_product needs for these sizes and results of `dtype`."""
     if a._device < 0 or a._device != w._device:
         raise ValueError("a, w: must be on one GPU")
     n = ctypes.c_size_t(0)
     with torch.cuda.device(a._device):
-        check(_lib.load().cora_rows_product_workspace(a._rows, w._rows, a._cols, ctypes.byref(n)),
-              "cora_rows_product_workspace")
+        check(_lib.load().cora_rows_product_workspace(a._rows, w._rows, a._cols, 1 if dtype is torch.float32 else 0,
+                                                       ctypes.byref(n)), "cora_rows_product_workspace")
     return n.value
 
 
@@ -673,22 +695,23 @@ def rows8_product(a: Rows8, w: Rows8, bias=None, dtype=torch.bfloat16, out=None,
     if out is None:
         if dtype not in (torch.bfloat16, torch.float32):
             raise TypeError(f"dtype: {dtype}, expected torch.bfloat16 or torch.float32")
-        out, ld = _empty((M, N), dtype, a._data.device, stream), N
+        out, ld = _empty((M, N), dtype, a._buffer.device, stream), N
     else:
         odev, ld = _rows_2d(out, "out", _STORED)
         if out.shape != (M, N) or odev != device:
             raise ValueError(f"out: shape {tuple(out.shape)} on {out.device}, the call needs [{M}, {N}] on cuda:{device}")
     if workspace is None:
-        key = (M, N, a._cols, device)
+        key = (M, N, a._cols, out.dtype, device)
         n = _product_workspaces.get(key)
         if n is None:
             if len(_product_workspaces) >= 256:
                 _product_workspaces.clear()
-            n = _product_workspaces[key] = rows8_product_workspace(a, w)
+            n = _product_workspaces[key] = rows8_product_workspace(a, w, out.dtype)
         if n:
             workspace = _empty(n, torch.uint8, out.device, stream)
+        at = None if workspace is None else workspace.data_ptr()
+    else:
+        at, n = _checked(workspace, "workspace", _U8, 0, device), workspace.numel()
     _call(device, "cora_rows_product", a._c, w._c, None if bias is None else _checked(bias, "bias", _F32, N, device),
-          out.data_ptr(), 1 if out.dtype is torch.float32 else 0, ld,
-          None if workspace is None else _checked(workspace, "workspace", _U8, 0, device),
-          0 if workspace is None else workspace.numel(), stream=stream)
+          out.data_ptr(), 1 if out.dtype is torch.float32 else 0, ld, at, n, stream=stream)
     return out

@@ -22,13 +22,10 @@ constexpr int BT = 512;         // threads of a range
 constexpr int BE = 16;          // logits of a thread and tile
 constexpr int TILE = BT * BE;
 constexpr int CAP = 1024;       // held candidates of a range
-constexpr int TRIM = 512;       // cut down to the W best beyond that
 constexpr float LOWEST = -3.3895313892515355e38f;  // bf16's lowest finite number
 // LOG2E's own error, relative: a sum of 2^(v LOG2E) is that of exp(v (1 + this)), which for the terms that count,
 // those near the largest, is a factor 1 + this times v
 constexpr double LOG2E_OFF = -1.3349e-8;
-
-struct __attribute__((packed, aligned(2))) bf16x8_any { uint16_t v[8]; };
 
 // order of a logit: larger for larger numbers, equal for both zeros, 0 for what is no candidate
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -42,25 +39,35 @@ __device__ __forceinline__ float of_ordered(uint32_t o) {
 __device__ __forceinline__ uint64_t candidate(uint32_t o, int id) { return (uint64_t)o << 32 | (0xffffffffu - (uint32_t)id); }
 __device__ __forceinline__ int id_of(uint64_t c) { return (int)(0xffffffffu - (uint32_t)c); }
 
-// The W largest of list[0 .. n) in falling order at its front; their number.  The list's rest is undefined.
+// The W largest of list[0 .. n) in falling order at its front; their number.  The list's rest is undefined; it has
+// room for eight more.  Eight are compared at a time (one after the other, each waits for its own load from LDS).
 __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t* least) {
+  const int tid = threadIdx.x;
+  if (tid < 8) list[n + tid] = 0;
+  __syncthreads();
   uint64_t own[CAP / BT];
   int rank[CAP / BT];
 #pragma unroll
   for (int e = 0; e < CAP / BT; ++e) {
-    const int at = threadIdx.x + e * BT;
-    own[e] = at < n ? list[at] : 0;
-    rank[e] = 0;
-  }
-  for (int i = 0; i < n; ++i) {
-    const uint64_t x = list[i];
+    own[e] = 0;
+    rank[e] = W;
+    if (tid + e * BT < n) {
+      own[e] = list[tid + e * BT];
+      int r = 0;
+      for (int i = 0; i < n; i += 8) {
+        uint64_t x[8];
 #pragma unroll
-    for (int e = 0; e < CAP / BT; ++e) rank[e] += x > own[e] ? 1 : 0;
+        for (int u = 0; u < 8; ++u) x[u] = list[i + u];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) r += x[u] > own[e] ? 1 : 0;
+      }
+      rank[e] = r;
+    }
   }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < CAP / BT; ++e)
-    if (threadIdx.x + e * BT < n && rank[e] < W) {
+    if (rank[e] < W) {
       list[rank[e]] = own[e];
       if (rank[e] == W - 1 && own[e]) *least = own[e];
     }
@@ -70,8 +77,10 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 
 }  // namespace
 
-__global__ __launch_bounds__(BT) void k_beam_rows(BeamArgs a) {
-  __shared__ uint64_t list[CAP];
+// Of a row's logits those in whole 16-byte blocks are loaded eight at a time, a tile ahead; the up to seven on either
+// side are one each of the first threads', before the first tile.
+__global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
+  __shared__ __attribute__((aligned(16))) uint64_t list[CAP + 8];
   __shared__ uint64_t least;      // candidates below it are out
   __shared__ int held;
   __shared__ uint64_t group_best[64];
@@ -81,62 +90,93 @@ __global__ __launch_bounds__(BT) void k_beam_rows(BeamArgs a) {
   const int part = blockIdx.x % a.parts;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;  // no candidates, or the one without logits
-  const int lo = part * a.chunk, hi = min(a.V, lo + a.chunk), W = a.W;
+  const int W = a.W, trim = max(64, 4 * W);  // held candidates beyond which they are cut down to the W best
   const uint16_t* x = a.logits + row * a.ld;
+  const int head = min(a.V, (int)(-((uintptr_t)x >> 1) & 7)), blocks = (a.V - head) / 8;
+  const int b0 = min(part * a.chunk, blocks), b1 = min(b0 + a.chunk, blocks);  // blocks of this range
+  const u32x4_t* body = reinterpret_cast<const u32x4_t*>(x + head);
   if (tid == 0) {
     least = 0x80ull << 32;  // LOWEST
     held = 0;
   }
-  __syncthreads();
 
   float ref = 0.f, k = LOG2E, o = 0.f, s = 0.f;
-  auto refer = [&](float m) {  // the power of two that the thread's terms are relative to
+  auto refer = [&](float m) {  // what the thread's terms are relative to: a power of two
     ref = fminf(fmaxf(m, LOWEST), -LOWEST);
-    k = fabsf(ref) >= 16384.f ? 1.f : LOG2E;  // from there on different bf16 numbers are 64 and more apart
+    k = fabsf(ref) >= 16384.f ? 1.f : LOG2E;  // from there on different bf16 numbers are 64 and more apart: 1 is as good
     o = k == 1.f ? -ref : -rintf(ref * LOG2E);
   };
-  for (int base = lo; base < hi; base += TILE) {
-    float v[BE];
-    float m8[BE / 8];
+  auto follow = [&](float m) {
+    if (!(m > ref + 60.f)) return;
+    const float was_k = k, was_o = o, was = ref;
+    refer(m);
+    s = was_k == LOG2E && k == LOG2E ? s * fast_exp2(o - was_o) : s * fast_exp2((was - ref) * LOG2E);
+  };
+
+  // the logit beside the blocks that this thread has, if any
+  int side = -1;
+  if (part == 0 && tid < head) side = tid;
+  if (part == a.parts - 1 && tid >= 8 && tid - 8 < a.V - head - 8 * blocks) side = head + 8 * blocks + tid - 8;
+  if (side == a.mask_id) side = -1;
+  const float sv = side >= 0 ? bf16_bits_to_f32(x[side]) : -INFINITY;
+
+  u32x4_t next[BE / 8];
+  auto load = [&](int at) {
+#pragma unroll
+    for (int h = 0; h < BE / 8; ++h) next[h] = body[min(at + h * BT + tid, b1 - 1)];
+  };
+  if (b0 < b1) load(b0);
+  uint64_t bound = 0x80ull << 32;
+  float bound_v = LOWEST;
+  for (int base = b0; base == b0 || base < b1; base += BT * BE / 8) {
+    float v[BE], m8[BE / 8];
+    const bool first = base == b0, any = b0 < b1;
+    if (any) {
+#pragma unroll
+      for (int h = 0; h < BE / 8; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[8 * h + 2 * e] = __uint_as_float(next[h][e] << 16);
+          v[8 * h + 2 * e + 1] = __uint_as_float(next[h][e] & 0xffff0000u);
+        }
+      load(min(base + BT * BE / 8, b1 - 1));  // past the last tile: not used
+    }
+    const int id0 = head + 8 * (base + tid);  // of v[0]; v[8 h] is BT * 8 h behind
+    if (base + BT * BE / 8 > b1 || (uint32_t)(a.mask_id - head - 8 * base) < (uint32_t)TILE) {  // the last tile, or the mask's
+#pragma unroll
+      for (int h = 0; h < BE / 8; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (base + h * BT + tid >= b1 || id0 + h * BT * 8 + e == a.mask_id) v[8 * h + e] = -INFINITY;
+    }
 #pragma unroll
     for (int h = 0; h < BE / 8; ++h) {
-      const int i = base + h * BT * 8 + tid * 8;
-      if (i + 8 <= hi) {
-        const bf16x8_any w = *reinterpret_cast<const bf16x8_any*>(x + i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * h + e] = bf16_bits_to_f32(w.v[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * h + e] = i + e < hi ? bf16_bits_to_f32(x[i + e]) : -INFINITY;
-      }
-      const uint32_t at = (uint32_t)(a.mask_id - i);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (at == (uint32_t)e) v[8 * h + e] = -INFINITY;
       m8[h] = v[8 * h];
 #pragma unroll
       for (int e = 1; e < 8; ++e) m8[h] = fmaxf(m8[h], v[8 * h + e]);
     }
-    const float m = fmaxf(m8[0], m8[1]);
-    if (base == lo) refer(m);
-    else if (m > ref + 60.f) {
-      const float was_k = k, was_o = o, was = ref;
-      refer(m);
-      s = was_k == LOG2E && k == LOG2E ? s * fast_exp2(o - was_o) : s * fast_exp2((was - ref) * LOG2E);
+    float m = m8[0];
+#pragma unroll
+    for (int h = 1; h < BE / 8; ++h) m = fmaxf(m, m8[h]);
+    if (first) {
+      refer(fmaxf(m, sv));
+      s = fast_exp2(fmaf(sv, k, o));
+    } else {
+      follow(m);
     }
 #pragma unroll
     for (int e = 0; e < BE; ++e) s += fast_exp2(fmaf(v[e], k, o));
 
-    if (base == lo) {
+    if (first) {
       // W of 64 groups of eight threads hold a logit no smaller than the W'th of the groups' largest
-      uint64_t best = 0;
+      int at_m = 0;  // the lowest place of the thread's largest
 #pragma unroll
-      for (int h = 0; h < BE / 8; ++h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint64_t c = candidate(ordered(v[8 * h + e]), base + h * BT * 8 + tid * 8 + e);
-          best = c > best ? c : best;
-        }
+      for (int e = BE - 1; e >= 0; --e) at_m = v[e] == m ? (e >> 3) * BT * 8 + (e & 7) : at_m;
+      uint64_t best = candidate(ordered(m), id0 + at_m);
+      if (side >= 0) {
+        const uint64_t c = candidate(ordered(sv), side);
+        best = c > best ? c : best;
+      }
 #pragma unroll
       for (int d = 1; d < 8; d <<= 1) {
         const uint64_t c = __shfl_xor((unsigned long long)best, d, 64);
@@ -144,41 +184,46 @@ __global__ __launch_bounds__(BT) void k_beam_rows(BeamArgs a) {
       }
       if ((lane & 7) == 0) group_best[tid >> 3] = best;
       __syncthreads();
-      if (wave == 0) {
-        const uint64_t mine = group_best[lane];
-        int rank = 0;
-        for (int j = 0; j < 64; ++j) rank += group_best[j] > mine || (group_best[j] == mine && j < lane) ? 1 : 0;
-        if (rank == W - 1 && mine > least) least = mine;
-      }
-      __syncthreads();
+      const uint64_t mine = group_best[lane];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < 64; ++j) rank += group_best[j] > mine || (group_best[j] == mine && j < lane) ? 1 : 0;
+      const uint64_t at = __ballot(rank == W - 1);
+      const uint64_t t = __shfl((unsigned long long)mine, __ffsll((unsigned long long)at) - 1, 64);
+      bound = t > bound ? t : bound;
+      bound_v = of_ordered((uint32_t)(bound >> 32));
+      if (tid == 0) least = bound;
+      if (side >= 0 && candidate(ordered(sv), side) >= bound) list[atomicAdd(&held, 1)] = candidate(ordered(sv), side);  // 14 at the most
     }
     auto offer = [&]() {
-      const uint64_t t = least;
-      const float tv = of_ordered((uint32_t)(t >> 32));
 #pragma unroll
       for (int h = 0; h < BE / 8; ++h) {
-        if (!(m8[h] >= tv)) continue;
+        if (!(m8[h] >= bound_v)) continue;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint64_t c = candidate(ordered(v[8 * h + e]), base + h * BT * 8 + tid * 8 + e);
-          if (c >= t) {
+          if (!(v[8 * h + e] >= bound_v)) continue;
+          const uint64_t c = candidate(ordered(v[8 * h + e]), id0 + h * BT * 8 + e);
+          if (c >= bound) {
             const int at = atomicAdd(&held, 1);
             if (at < CAP) list[at] = c;
           }
         }
       }
     };
+    auto cut = [&](int n) {
+      n = keep_best(list, n, W, &least);
+      bound = least;
+      bound_v = of_ordered((uint32_t)(bound >> 32));
+      return n;
+    };
     offer();
     __syncthreads();
     int n = held;
     while (n > CAP) {  // more than fit: the bound of those that do, then this tile's again
-      uint64_t mine[CAP / BT];
-      keep_best(list, CAP, W, &least);
-#pragma unroll
-      for (int e = 0; e < CAP / BT; ++e) {
-        const int at = tid + e * BT;
-        mine[e] = at < W ? list[at] : 0;
-        if (at < W && id_of(mine[e]) >= base) list[at] = 0;
+      cut(CAP);
+      for (int i = tid; i < W; i += BT) {
+        const int id = id_of(list[i]);
+        if (id >= head + 8 * base && id < head + 8 * b1) list[i] = 0;
       }
       if (tid == 0) held = W;
       __syncthreads();
@@ -186,8 +231,8 @@ __global__ __launch_bounds__(BT) void k_beam_rows(BeamArgs a) {
       __syncthreads();
       n = held;
     }
-    if (n > TRIM) {
-      n = keep_best(list, n, W, &least);
+    if (n > trim) {
+      n = cut(n);
       if (tid == 0) held = n;
     }
     __syncthreads();
@@ -219,40 +264,53 @@ __global__ __launch_bounds__(BT) void k_beam_rows(BeamArgs a) {
 
 namespace {
 
-struct Scored {
-  double score;
-  uint64_t which;
-  int row;
-};
-__device__ __forceinline__ bool before(double s, int row, uint64_t which, double t, int row2, uint64_t which2) {
-  return s > t || (s == t && (row < row2 || (row == row2 && which > which2)));
+// A candidate in order: its score's, then lower beams first, then its order in the row; 0 is none.
+typedef uint64_t key_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ key_t key_of(double score, int beam, uint64_t which) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, score + 0.0);
+  return key_t{b >> 63 ? ~b : b | 1ull << 63, (uint64_t)(63 - beam) << 48 | which};
+}
+__device__ __forceinline__ double score_of(key_t k) {
+  return __builtin_bit_cast(double, k[0] >> 63 ? k[0] ^ 1ull << 63 : ~k[0]);
+}
+__device__ __forceinline__ bool before(key_t x, key_t y) { return x[0] > y[0] || (x[0] == y[0] && x[1] > y[1]); }
+// how many of n keys come before one; the list has room for four more, which are none
+__device__ __forceinline__ int rank_of(const key_t* keys, int n, key_t mine) {
+  int r = 0;
+  for (int i = 0; i < n; i += 4) {
+    key_t x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = keys[i + u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) r += before(x[u], mine) ? 1 : 0;
+  }
+  return r;
 }
 
 }  // namespace
 
-constexpr int MT = 512;
+static_assert(BEAM_MAX <= 64, "a beam's number in six bits above a candidate's 48");
 
-__global__ __launch_bounds__(MT) void k_beam_merge(BeamArgs a) {
-  extern __shared__ char mem[];
+// Bound by latency: loads of the ranges' numbers, a logarithm a beam, and ranks by comparing all with all.
+__global__ __launch_bounds__(512) void k_beam_merge(BeamArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char mem[];
   const int tid = threadIdx.x, K = a.K, P = a.parts, W = a.W, lists = K * P;
   const int64_t row0 = (int64_t)blockIdx.x * K;
-  double* base = reinterpret_cast<double*>(mem);               // [K] score minus the log of the row's sum; NaN: no candidate
-  double* origin = base + K;                                   // [K] which is relative to this (logits of 1e38 keep the score's bits)
-  double* score = origin + K;                                    // [W W] of the candidates that may be in
-  uint64_t* which = reinterpret_cast<uint64_t*>(score + W * W);
-  int* row = reinterpret_cast<int*>(which + W * W);
-  double* head = reinterpret_cast<double*>(row + W * W + (W * W & 1));  // [lists]
+  key_t* keys = reinterpret_cast<key_t*>(mem);          // [max(W W, lists) + 4]
+  double* base = reinterpret_cast<double*>(keys + max(W * W, lists) + 4);  // [K] score minus the log of the row's sum; NaN: no candidate
+  double* origin = base + K;                            // [K] which is relative to this (logits of 1e38 keep the score's bits)
   __shared__ int n_in;
-  __shared__ Scored least;
+  __shared__ key_t least;
   if (tid == 0) {
     n_in = 0;
-    least = Scored{-INFINITY, 0, INT_MAX};
+    least = key_t{0, 0};
   }
-  for (int k = tid; k < K; k += MT) {
+  auto is_done = [&](int k) { return a.done && a.done[row0 + k]; };
+  for (int k = tid; k < K; k += 512) {
     const double s = a.score[row0 + k];
     double b = __builtin_nan(""), top = 0;
-    if (s > -INFINITY) {
-      if (a.done && a.done[row0 + k]) {
+    if (s > -INFINITY && s < INFINITY) {
+      if (is_done(k)) {
         b = s;
       } else {
         const double* st = a.stats + 2 * (row0 + k) * P;
@@ -267,86 +325,60 @@ __global__ __launch_bounds__(MT) void k_beam_merge(BeamArgs a) {
     origin[k] = top;
   }
   __syncthreads();
-  auto is_done = [&](int k) { return a.done && a.done[row0 + k]; };
   // candidate i of list l (a beam's range), in the list's falling order
-  auto get = [&](int l, int i, double& s, uint64_t& w) {
+  auto get = [&](int l, int i) {
     const int k = l / P;
-    if (!(base[k] == base[k]) || !(base[k] < INFINITY)) return false;
-    if (is_done(k)) {
-      s = base[k];
-      w = 1;
-      return l % P == 0 && i == 0;
-    }
-    w = a.best[((row0 + k) * P + l % P) * W + i];
-    s = base[k] + ((double)of_ordered((uint32_t)(w >> 32)) - origin[k]);
-    return w != 0;
+    const double b = base[k];
+    if (!(b == b)) return key_t{0, 0};
+    if (is_done(k)) return l % P == 0 && i == 0 ? key_of(b, k, 1) : key_t{0, 0};
+    const uint64_t w = a.best[((row0 + k) * P + l % P) * W + i];
+    return w ? key_of(b + ((double)of_ordered((uint32_t)(w >> 32)) - origin[k]), k, w) : key_t{0, 0};
   };
-  // the W'th largest head of the lists: a candidate before that many others at least
+  // the W'th of the lists' heads: a candidate behind it has that many others before it
   if (lists > W) {
-    for (int l = tid; l < lists; l += MT) {
-      double s;
-      uint64_t w;
-      head[l] = get(l, 0, s, w) ? s : -INFINITY;
+    for (int l = tid; l < lists + 4; l += 512) keys[l] = l < lists ? get(l, 0) : key_t{0, 0};
+    __syncthreads();
+    for (int l = tid; l < lists; l += 512) {
+      const key_t mine = keys[l];
+      if (mine[0] && rank_of(keys, lists, mine) == W - 1) least = mine;
     }
     __syncthreads();
-    for (int l = tid; l < lists; l += MT) {
-      double s;
-      uint64_t w;
-      if (!get(l, 0, s, w)) continue;
-      int rank = 0;
-      for (int j = 0; j < lists; ++j) {
-        if (head[j] > s) ++rank;
-        else if (head[j] == s && j != l) {
-          double t;
-          uint64_t u;
-          if (get(j, 0, t, u) && before(t, j / P, u, s, l / P, w)) ++rank;
-        }
-      }
-      if (rank == W - 1) least = Scored{s, w, l / P};
-    }
+  }
+  const key_t bound = least;
+  __syncthreads();
+  for (int c = tid; c < lists * W; c += 512) {
+    const key_t mine = get(c / W, c % W);
+    if (mine[0] && !before(bound, mine)) keys[atomicAdd(&n_in, 1)] = mine;  // W lists of W at the most
   }
   __syncthreads();
-  const Scored lim = least;
-  for (int c = tid; c < lists * W; c += MT) {
-    const int l = c / W;
-    double s;
-    uint64_t w;
-    if (!get(l, c % W, s, w) || !(s > -INFINITY)) continue;
-    if (lim.row != INT_MAX && before(lim.score, lim.row, lim.which, s, l / P, w)) continue;
-    const int at = atomicAdd(&n_in, 1);
-    if (at < W * W) {
-      score[at] = s;
-      which[at] = w;
-      row[at] = l / P;
-    }
-  }
+  const int n = n_in;
+  if (tid < 4) keys[n + tid] = key_t{0, 0};
   __syncthreads();
-  const int n = min(n_in, W * W);
   const int64_t out = (int64_t)blockIdx.x * W;
-  for (int c = tid; c < n; c += MT) {
-    const double s = score[c];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += before(score[j], row[j], which[j], s, row[c], which[c]) ? 1 : 0;
+  for (int c = tid; c < n; c += 512) {
+    const key_t mine = keys[c];
+    const int rank = rank_of(keys, n, mine), k = 63 - (int)(mine[1] >> 48);
     if (rank < W) {
-      a.token[out + rank] = is_done(row[c]) ? a.done_token : id_of(which[c]);
-      a.parent[out + rank] = (int)(row0 + row[c]);
-      a.next[out + rank] = (float)s;
+      a.token[out + rank] = is_done(k) ? a.done_token : id_of(mine[1]);
+      a.parent[out + rank] = (int)(row0 + k);
+      a.next[out + rank] = (float)score_of(mine);
     }
   }
-  for (int c = n + tid; c < W; c += MT) {
+  for (int c = n + tid; c < W; c += 512) {
     a.token[out + c] = -1;
     a.parent[out + c] = -1;
     a.next[out + c] = -INFINITY;
   }
 }
 
-// Ranges of a row: enough workgroups for the chip, ranges of a tile at the least.
+// Ranges of a row: enough workgroups for the chip, ranges of a tile at the least; in blocks of eight ids.
 BeamPlan beam_plan(int B, int K, int V, int W, int num_cus) {
   const int64_t rows = (int64_t)B * K;
   int64_t parts = std::max<int64_t>(1, std::min<int64_t>(4 * num_cus / std::max<int64_t>(rows, 1), (V + TILE - 1) / TILE));
   BeamPlan p;
-  p.chunk = (int)(((V + parts - 1) / parts + 7) / 8 * 8);
-  p.parts = (V + p.chunk - 1) / p.chunk;
+  const int blocks = std::max(1, V / 8);
+  p.chunk = (int)((blocks + parts - 1) / parts);
+  p.parts = (blocks + p.chunk - 1) / p.chunk;
   p.bytes = (size_t)rows * p.parts * (16 + 8 * (size_t)W);
   return p;
 }
@@ -358,8 +390,8 @@ hipError_t launch_vocab_beam(BeamArgs a, const BeamPlan& p, void* ws, hipStream_
   a.best = reinterpret_cast<uint64_t*>(a.stats + 2 * (size_t)a.B * a.K * a.parts);
   hipLaunchKernelGGL(k_beam_rows, dim3((unsigned)((int64_t)a.B * a.K * a.parts)), dim3(BT), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  const size_t lds = 16 * (size_t)a.K + 20 * (size_t)a.W * a.W + 8 + 8 * (size_t)a.K * a.parts;
-  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.B), dim3(MT), lds, s, a);
+  const size_t lds = 16 * ((size_t)std::max(a.W * a.W, a.K * a.parts) + 4 + a.K);
+  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.B), dim3(512), lds, s, a);
   return hipGetLastError();
 }
 

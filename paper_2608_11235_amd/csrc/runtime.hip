@@ -1326,11 +1326,10 @@ static cora_status check_product_sizes(int32_t M, int32_t N, int32_t cols) {
   return CORA_OK;
 }
 
-extern "C" cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, size_t* bytes) try {
+extern "C" cora_status cora_rows_product_workspace(int32_t M, int32_t N, int32_t cols, int32_t out_f32, size_t* bytes) try {
   if (!bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
   if (cora_status e = check_product_sizes(M, N, cols)) return e;
-  const int cus = current_cus();  // enough for either type of result
-  *bytes = 4 * std::max(rows8_plan(M, N, cols, false, cus).ws_floats, rows8_plan(M, N, cols, true, cus).ws_floats);
+  *bytes = 4 * rows8_plan(M, N, cols, out_f32 != 0, current_cus()).ws_floats;
   return CORA_OK;
 } catch (...) {
   return exception_status();

@@ -59,19 +59,22 @@ def test_sizes(lib):  # noqa: F811
         assert f(R, K, ctypes.byref(d), ctypes.byref(s)) == 0 and (d.value, s.value) == want
     assert f(1, 0, ctypes.byref(d), ctypes.byref(s)) == INVALID and f(1, 1, None, ctypes.byref(s)) == INVALID
     g = lib.load().cora_rows_product_workspace
-    assert g(32, 4096, 4096, ctypes.byref(d)) == 0
-    assert g(32, 4096, 4096, None) == INVALID and g(32, 4096, 0, ctypes.byref(d)) == INVALID
-    assert g(32, (1 << 25) + 1, 64, ctypes.byref(d)) == UNSUPPORTED
+    assert g(32, 4096, 4096, 0, ctypes.byref(d)) == 0
+    assert g(32, 4096, 4096, 1, None) == INVALID and g(32, 4096, 0, 0, ctypes.byref(d)) == INVALID
+    assert g(32, (1 << 25) + 1, 64, 0, ctypes.byref(d)) == UNSUPPORTED
 
 
 def test_product_workspace_is_checked(lib):  # noqa: F811
     n = ctypes.c_size_t(0)
-    for M in (32, 128, 300):
-        assert lib.load().cora_rows_product_workspace(M, 4096, 4096, ctypes.byref(n)) == 0
+    seen = 0
+    for M, N, K, f32 in ((32, 4096, 12288, 0), (32, 4096, 12288, 1), (512, 4096, 12288, 0), (300, 256, 4096, 1), (64, 3584, 18944, 0)):
+        assert lib.load().cora_rows_product_workspace(M, N, K, f32, ctypes.byref(n)) == 0
         if n.value:
-            a, w = rows8(lib, rows=M, cols=4096), rows8(lib, rows=4096, cols=4096)
-            assert product(lib, a, w, ws=None) == INVALID and product(lib, a, w, ws=FAKE + 8) == INVALID
-            assert product(lib, a, w, n=n.value - 1) == INVALID
+            a, w = rows8(lib, rows=M, cols=K), rows8(lib, rows=N, cols=K)
+            assert product(lib, a, w, f32=f32, ws=None) == INVALID and product(lib, a, w, f32=f32, ws=FAKE + 8) == INVALID
+            assert product(lib, a, w, f32=f32, n=n.value - 1) == INVALID
+            seen += 1
+    assert seen >= 3
 
 
 def test_layout_matches_the_header(lib, tmp_path):  # noqa: F811
