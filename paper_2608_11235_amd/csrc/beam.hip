@@ -18,10 +18,10 @@ namespace cora {
 
 namespace {
 
-constexpr int BT = 512;         // threads of a range
+constexpr int BT = 256;         // threads of a range
 constexpr int BE = 16;          // logits of a thread and tile
 constexpr int TILE = BT * BE;
-constexpr int CAP = 1024;       // held candidates of a range
+constexpr int CAP = 512;       // held candidates of a range
 constexpr float LOWEST = -3.3895313892515355e38f;  // bf16's lowest finite number
 // LOG2E's own error, relative: a sum of 2^(v LOG2E) is that of exp(v (1 + this)), which for the terms that count,
 // those near the largest, is a factor 1 + this times v
@@ -40,10 +40,10 @@ __device__ __forceinline__ uint64_t candidate(uint32_t o, int id) { return (uint
 __device__ __forceinline__ int id_of(uint64_t c) { return (int)(0xffffffffu - (uint32_t)c); }
 
 // The W largest of list[0 .. n) in falling order at its front; their number.  The list's rest is undefined; it has
-// room for eight more.  Eight are compared at a time (one after the other, each waits for its own load from LDS).
+// room for four more.  Four are compared at a time (one after the other, each waits for its own load from LDS).
 __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t* least) {
   const int tid = threadIdx.x;
-  if (tid < 8) list[n + tid] = 0;
+  if (tid < 4) list[n + tid] = 0;
   __syncthreads();
   uint64_t own[CAP / BT];
   int rank[CAP / BT];
@@ -54,12 +54,12 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
     if (tid + e * BT < n) {
       own[e] = list[tid + e * BT];
       int r = 0;
-      for (int i = 0; i < n; i += 8) {
-        uint64_t x[8];
+      for (int i = 0; i < n; i += 4) {
+        uint64_t x[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = list[i + u];
+        for (int u = 0; u < 4; ++u) x[u] = list[i + u];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) r += x[u] > own[e] ? 1 : 0;
+        for (int u = 0; u < 4; ++u) r += x[u] > own[e] ? 1 : 0;
       }
       rank[e] = r;
     }
@@ -77,13 +77,15 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 
 }  // namespace
 
+// Bound by its instructions, eight a logit, of them one exponential: 1024 x 152064 in 72 us (4.3 TB/s) with four workgroups of
+// 256 threads a CU (two of 512: 80; a second tile ahead: 76; 32 logits a thread: 105, in scratch memory).
 // Of a row's logits those in whole 16-byte blocks are loaded eight at a time, a tile ahead; the up to seven on either
 // side are one each of the first threads', before the first tile.
 __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
-  __shared__ __attribute__((aligned(16))) uint64_t list[CAP + 8];
+  __shared__ __attribute__((aligned(16))) uint64_t list[CAP + 4];
   __shared__ uint64_t least;      // candidates below it are out
   __shared__ int held;
-  __shared__ uint64_t group_best[64];
+  __shared__ uint64_t group_best[64];  // of BT / 64 threads each
   __shared__ double sums[BT / 64], tops[BT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x / a.parts;
@@ -120,40 +122,40 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   if (side == a.mask_id) side = -1;
   const float sv = side >= 0 ? bf16_bits_to_f32(x[side]) : -INFINITY;
 
-  u32x4_t next[BE / 8];
-  auto load = [&](int at) {
+  u32x4_t next[BE / 8] = {};
+  auto load = [&](int at, bool any) {
+    if (!any) return;
 #pragma unroll
     for (int h = 0; h < BE / 8; ++h) next[h] = body[min(at + h * BT + tid, b1 - 1)];
   };
-  if (b0 < b1) load(b0);
+  load(b0, b0 < b1);
   uint64_t bound = 0x80ull << 32;
   float bound_v = LOWEST;
   for (int base = b0; base == b0 || base < b1; base += BT * BE / 8) {
-    float v[BE], m8[BE / 8];
+    u32x4_t cur[BE / 8];
+    float m8[BE / 8];
     const bool first = base == b0, any = b0 < b1;
-    if (any) {
+    const int id0 = head + 8 * (base + tid);  // of the first logit; those of cur[h] are BT * 8 h behind
 #pragma unroll
-      for (int h = 0; h < BE / 8; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[8 * h + 2 * e] = __uint_as_float(next[h][e] << 16);
-          v[8 * h + 2 * e + 1] = __uint_as_float(next[h][e] & 0xffff0000u);
-        }
-      load(min(base + BT * BE / 8, b1 - 1));  // past the last tile: not used
-    }
-    const int id0 = head + 8 * (base + tid);  // of v[0]; v[8 h] is BT * 8 h behind
+    for (int h = 0; h < BE / 8; ++h) cur[h] = next[h];
+    load(min(base + BT * BE / 8, max(b1 - 1, 0)), any);  // past the last tile: not used
     if (base + BT * BE / 8 > b1 || (uint32_t)(a.mask_id - head - 8 * base) < (uint32_t)TILE) {  // the last tile, or the mask's
 #pragma unroll
-      for (int h = 0; h < BE / 8; ++h)
+      for (int h = 0; h < BE / 8; ++h) {
+        int at = base + h * BT + tid >= b1 ? INT_MIN : a.mask_id - id0 - h * BT * 8;  // which of the eight is out; INT_MIN: all
+        asm volatile("" : "+v"(at));
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (base + h * BT + tid >= b1 || id0 + h * BT * 8 + e == a.mask_id) v[8 * h + e] = -INFINITY;
+          if (at == e || at == INT_MIN)
+            cur[h][e >> 1] = e & 1 ? (cur[h][e >> 1] & 0xffffu) | 0xff800000u : (cur[h][e >> 1] & 0xffff0000u) | 0xff80u;
+      }
     }
+    auto logit = [&](int h, int e) { return __uint_as_float(e & 1 ? cur[h][e >> 1] & 0xffff0000u : cur[h][e >> 1] << 16); };
 #pragma unroll
     for (int h = 0; h < BE / 8; ++h) {
-      m8[h] = v[8 * h];
+      m8[h] = logit(h, 0);
 #pragma unroll
-      for (int e = 1; e < 8; ++e) m8[h] = fmaxf(m8[h], v[8 * h + e]);
+      for (int e = 1; e < 8; ++e) m8[h] = fmaxf(m8[h], logit(h, e));
     }
     float m = m8[0];
 #pragma unroll
@@ -165,24 +167,24 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
       follow(m);
     }
 #pragma unroll
-    for (int e = 0; e < BE; ++e) s += fast_exp2(fmaf(v[e], k, o));
+    for (int e = 0; e < BE; ++e) s += fast_exp2(fmaf(logit(e >> 3, e & 7), k, o));
 
     if (first) {
-      // W of 64 groups of eight threads hold a logit no smaller than the W'th of the groups' largest
+      // W of 64 groups of threads hold a logit no smaller than the W'th of the groups' largest
       int at_m = 0;  // the lowest place of the thread's largest
 #pragma unroll
-      for (int e = BE - 1; e >= 0; --e) at_m = v[e] == m ? (e >> 3) * BT * 8 + (e & 7) : at_m;
+      for (int e = BE - 1; e >= 0; --e) at_m = logit(e >> 3, e & 7) == m ? (e >> 3) * BT * 8 + (e & 7) : at_m;
       uint64_t best = candidate(ordered(m), id0 + at_m);
       if (side >= 0) {
         const uint64_t c = candidate(ordered(sv), side);
         best = c > best ? c : best;
       }
 #pragma unroll
-      for (int d = 1; d < 8; d <<= 1) {
+      for (int d = 1; d < BT / 64; d <<= 1) {
         const uint64_t c = __shfl_xor((unsigned long long)best, d, 64);
         best = c > best ? c : best;
       }
-      if ((lane & 7) == 0) group_best[tid >> 3] = best;
+      if (tid % (BT / 64) == 0) group_best[tid / (BT / 64)] = best;
       __syncthreads();
       const uint64_t mine = group_best[lane];
       int rank = 0;
@@ -199,10 +201,13 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
 #pragma unroll
       for (int h = 0; h < BE / 8; ++h) {
         if (!(m8[h] >= bound_v)) continue;
+        int id = id0 + h * BT * 8;
+        asm volatile("" : "+v"(id));  // made here: eight ids made before the branch cost a workgroup its place on the CU
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if (!(v[8 * h + e] >= bound_v)) continue;
-          const uint64_t c = candidate(ordered(v[8 * h + e]), id0 + h * BT * 8 + e);
+          const float v = logit(h, e);
+          if (!(v >= bound_v)) continue;
+          const uint64_t c = candidate(ordered(v), id + e);
           if (c >= bound) {
             const int at = atomicAdd(&held, 1);
             if (at < CAP) list[at] = c;
