@@ -464,6 +464,23 @@ cora_status cora_rows_product(const cora_rows8 *a, const cora_rows8 *w, const fl
                                void *d_out, int32_t out_f32, int64_t ld, void *workspace,
                                size_t workspace_bytes, void *hip_stream);
 
+/* The layers' matrices in 8 bits, in memory of the caller's (256-byte aligned, cora_model_quantized_bytes
+ * bytes, their layout the library's): cora_model_quantize rounds them, each row's blocks of 128 columns as
+ * cora_quantize_rows does.  Embedding, biases and LM head stay as they are.  cora_forward_quantized is
+ * cora_forward_cached on these: the inputs of the four products of a layer (normalised rows, attention output,
+ * normalised rows, silu(gate) * up of the bf16 results) are rounded to 8 bits alike, the sums are fp32.  One cache serves
+ * both passes.  Splits and tiles follow chunk->rows alone.  workspace of cora_forward_quantized_workspace bytes,
+ * 256-byte aligned: used from this call's start to its end on the stream, like the model's workspace, which it uses too.
+ * Asynchronous. */
+cora_status cora_model_quantized_bytes(cora_model *model, size_t *bytes);
+cora_status cora_model_quantize(cora_model *model, void *d_weights, size_t bytes, void *hip_stream);
+cora_status cora_forward_quantized_workspace(cora_model *model, int32_t rows, size_t *bytes);
+cora_status cora_forward_quantized(cora_model *model, const void *d_weights, size_t weights_bytes,
+                                   const cora_cache *cache, const cora_pages *pages,
+                                   const cora_chunk *chunk, const int32_t *d_tokens, int32_t max_count,
+                                   int32_t max_len, int32_t causal, uint16_t *d_logits, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
 /* Copy weight tensor `tensor_id` (ids as in cora_model_create) to host memory
  * in its logical row-major [out, in] layout as bf16 bits (biases too).
  * `bytes` must equal the tensor's size.  Synchronous. */

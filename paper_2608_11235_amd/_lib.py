@@ -96,6 +96,11 @@ EXPORTS = {
     "cora_vocab_beam_workspace": (c_i32, [c_i32, c_i32, c_i32, c_i32, _P(c_sz)]),
     "cora_vocab_beam": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i64, c_i32, c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, c_vp,
                                 c_vp, c_sz, c_vp]),
+    "cora_model_quantized_bytes": (c_i32, [c_vp, _P(c_sz)]),
+    "cora_model_quantize": (c_i32, [c_vp, c_vp, c_sz, c_vp]),
+    "cora_forward_quantized_workspace": (c_i32, [c_vp, c_i32, _P(c_sz)]),
+    "cora_forward_quantized": (c_i32, [c_vp, c_vp, c_sz, _P(Cache), _P(Pages), _P(ChunkRows), c_vp, c_i32, c_i32, c_i32,
+                                       c_vp, c_vp, c_sz, c_vp]),
     "cora_rows_bytes": (c_i32, [c_i32, c_i32, _P(c_sz), _P(c_sz)]),
     "cora_quantize_rows": (c_i32, [c_vp, c_i32, c_i64, _P(Rows8), c_vp]),
     "cora_rows_product_workspace": (c_i32, [c_i32, c_i32, c_i32, c_i32, _P(c_sz)]),

@@ -139,6 +139,7 @@ class Model:
                                     stream_handle(stream), ctypes.byref(h)), "cora_model_create")
         self._h = h
         self._device = torch.cuda.current_device()
+        self._quantized_workspaces = {}  # bytes that a pass on 8-bit weights needs, by its rows
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -196,10 +197,34 @@ class Model:
               "cora_block_decode")
         return out, passes, int(total.value)
 
+    def quantize(self, out=None, stream=None):
+        """The layers' matrices in 8 bits, for forward_cached (cora_model_quantize): a uint8 tensor."""
+        n = ctypes.c_size_t(0)
+        check(_lib.load().cora_model_quantized_bytes(self._h, ctypes.byref(n)), "cora_model_quantized_bytes")
+        if out is None:
+            out = _empty(n.value, torch.uint8, torch.device("cuda", self._device), stream)
+        _call(self._device, "cora_model_quantize", self._h, _checked(out, "out", _U8, n.value, self._device), out.numel(),
+              stream=stream)
+        return out
+
+    def quantized_workspace(self, rows):
+        """Bytes of workspace that forward_cached needs for a chunk of `rows` on 8-bit weights."""
+        n = self._quantized_workspaces.get(rows)
+        if n is None:
+            got = ctypes.c_size_t(0)
+            check(_lib.load().cora_forward_quantized_workspace(self._h, rows, ctypes.byref(got)),
+                  "cora_forward_quantized_workspace")
+            if len(self._quantized_workspaces) >= 256:
+                self._quantized_workspaces.clear()
+            n = self._quantized_workspaces[rows] = got.value
+        return n
+
     def forward_cached(self, cache, chunk, tokens, max_count=0, max_len=0, causal=False, out=None,
-                       stream=None):
+                       stream=None, weights=None, workspace=None):
         """Logits [chunk.rows, vocab] (bf16 bits) of a planned chunk against the cache, whose pages
-        receive the chunk's K and V (cora_forward_cached)."""
+        receive the chunk's K and V (cora_forward_cached).  weights: what quantize returned, for products in 8
+        bits (cora_forward_quantized), with a workspace of quantized_workspace(chunk.rows) bytes, by default from
+        torch's allocator for the call."""
         device = _device_of(cache, chunk)
         if device != self._device:
             raise ValueError(f"cache: on cuda:{device}, the model is on cuda:{self._device}")
@@ -207,6 +232,14 @@ class Model:
         at = _checked(tokens, "tokens", _I32, rows, device)
         if out is None:
             out = _empty((rows, vocab), torch.int16, tokens.device, stream)
+        if weights is not None:
+            if workspace is None:
+                workspace = _empty(self.quantized_workspace(rows), torch.uint8, tokens.device, stream)
+            _call(device, "cora_forward_quantized", self._h, _checked(weights, "weights", _U8, 0, device), weights.numel(),
+                  cache._cache, cache._pages, chunk._chunk, at, max_count, max_len, 1 if causal else 0,
+                  _checked(out, "out", _BF16_BITS, rows * vocab, device), _checked(workspace, "workspace", _U8, 0, device),
+                  workspace.numel(), stream=stream)
+            return out
         _call(device, "cora_forward_cached", self._h, cache._cache, cache._pages, chunk._chunk, at, max_count,
               max_len, 1 if causal else 0, _checked(out, "out", _BF16_BITS, rows * vocab, device), stream=stream)
         return out

@@ -26,10 +26,22 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 struct __attribute__((packed, aligned(2))) bf16x8_any { uint16_t v[8]; };
 struct __attribute__((packed, aligned(4))) f32x4_any { float v[4]; };
 
+__device__ __forceinline__ void unpack16(const uint16_t* p, float (&x)[16]) {  // aligned to 16 bytes
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p + 8 * t);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[8 * t + 2 * i] = __uint_as_float(v[i] << 16);
+      x[8 * t + 2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  }
+}
+
 // columns c0 .. c0 + 15 of a row, zeros from column K on
-template <bool F32>
+template <R8Source FROM>
 __device__ __forceinline__ void load_chunk(const QuantizeArgs& a, int64_t row, int c0, float (&x)[16]) {
-  if constexpr (F32) {
+  if constexpr (FROM == R8_F32) {
     const float* p = static_cast<const float*>(a.x) + row * a.ld + c0;
     if (c0 + 16 <= a.cols) {
 #pragma unroll
@@ -42,7 +54,7 @@ __device__ __forceinline__ void load_chunk(const QuantizeArgs& a, int64_t row, i
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = c0 + i < a.cols ? p[i] : 0.f;
-  } else {
+  } else if constexpr (FROM == R8_BF16) {
     const uint16_t* p = static_cast<const uint16_t*>(a.x) + row * a.ld + c0;
     if (c0 + 16 <= a.cols) {
 #pragma unroll
@@ -55,6 +67,22 @@ __device__ __forceinline__ void load_chunk(const QuantizeArgs& a, int64_t row, i
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = c0 + i < a.cols ? bf16_bits_to_f32(p[i]) : 0.f;
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(a.x);
+    if (c0 >= a.cols) {  // cols % 16 == 0
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    } else if constexpr (FROM == R8_BLOCKS) {
+      unpack16(p + ((row >> 6) * (a.cols >> 5) + (c0 >> 5)) * 2048 + (row & 63) * 32 + (c0 & 31), x);
+    } else if constexpr (FROM == R8_PANELS) {
+      unpack16(p + ((int64_t)(c0 >> 5) * a.rows + row) * 32 + (c0 & 31), x);
+    } else {
+      float up[16];
+      unpack16(p + row * a.ld + 2 * c0, x);
+      unpack16(p + row * a.ld + 2 * c0 + 16, up);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = x[i] / (1.0f + __expf(-x[i])) * up[i];
+    }
   }
 }
 
@@ -81,7 +109,7 @@ __device__ __forceinline__ u32x4_t pack_e4m3(const float (&x)[16], float by) {
 }  // namespace
 
 // A thread has 16 columns of one row, eight neighbouring threads a block's row, two wavefronts a block.
-template <bool F32>
+template <R8Source FROM>
 __global__ __launch_bounds__(512) void k_quantize_rows(QuantizeArgs a) {
   const int tid = threadIdx.x, c = tid & 7, r = (tid >> 3) & 15;
   const int nk = r8_blocks(a.cols), nq = r8_quads(a.cols), quad = blockIdx.x % nq, kb = quad * 4 + (tid >> 7);
@@ -89,7 +117,7 @@ __global__ __launch_bounds__(512) void k_quantize_rows(QuantizeArgs a) {
   float x[16];
   uint32_t most = 0;
   if (row < a.rows && kb < nk) {
-    load_chunk<F32>(a, row, kb * 128 + c * 16, x);
+    load_chunk<FROM>(a, row, kb * 128 + c * 16, x);
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
@@ -110,10 +138,15 @@ __global__ __launch_bounds__(512) void k_quantize_rows(QuantizeArgs a) {
   if (c == 0) a.scale[(group * nq + quad) * 64 + r * 4 + (tid >> 7)] = (uint8_t)e;
 }
 
-hipError_t launch_quantize_rows(const QuantizeArgs& a, bool f32, hipStream_t s) {
+hipError_t launch_quantize_rows(const QuantizeArgs& a, R8Source from, hipStream_t s) {
   const dim3 grid((unsigned)(r8_groups(a.rows) * r8_quads(a.cols)));  // below 2^23
-  if (f32) hipLaunchKernelGGL((k_quantize_rows<true>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((k_quantize_rows<false>), grid, dim3(512), 0, s, a);
+  switch (from) {
+    case R8_BF16: hipLaunchKernelGGL(k_quantize_rows<R8_BF16>, grid, dim3(512), 0, s, a); break;
+    case R8_F32: hipLaunchKernelGGL(k_quantize_rows<R8_F32>, grid, dim3(512), 0, s, a); break;
+    case R8_BLOCKS: hipLaunchKernelGGL(k_quantize_rows<R8_BLOCKS>, grid, dim3(512), 0, s, a); break;
+    case R8_PANELS: hipLaunchKernelGGL(k_quantize_rows<R8_PANELS>, grid, dim3(512), 0, s, a); break;
+    case R8_SWIGLU: hipLaunchKernelGGL(k_quantize_rows<R8_SWIGLU>, grid, dim3(512), 0, s, a); break;
+  }
   return hipGetLastError();
 }
 

@@ -19,12 +19,18 @@ __host__ __device__ inline int r8_quads(int cols) { return (cols + 511) / 512; }
 constexpr int R8_MAX_COLS = 1 << 20, R8_MAX_ROWS = 1 << 27;
 constexpr int R8_MAX_PRODUCT_ROWS = 1 << 21, R8_MAX_PRODUCT_COLS = 1 << 25;  // a launch's workgroups
 
+// Where the quantized rows come from: bf16 or fp32 rows of stride ld; a layer's weights in 64 x 32 blocks; K panels
+// [cols / 32][rows][32] (cols % 32 == 0 in both); or silu(gate) * up of bf16 rows that hold 16 gate and 16 up
+// columns in turn.
+enum R8Source { R8_BF16, R8_F32, R8_BLOCKS, R8_PANELS, R8_SWIGLU };
 struct QuantizeArgs {
-  const void* x; int64_t ld;  // bf16, or fp32
+  const void* x; int64_t ld;
   int rows, cols;
   uint8_t *data, *scale;
 };
-hipError_t launch_quantize_rows(const QuantizeArgs& a, bool f32, hipStream_t s);
+hipError_t launch_quantize_rows(const QuantizeArgs& a, R8Source from, hipStream_t s);
+inline size_t r8_data_bytes(int64_t rows, int cols) { return (size_t)r8_groups(rows) * r8_blocks(cols) * R8_BLOCK; }
+inline size_t r8_scale_bytes(int64_t rows, int cols) { return (size_t)r8_groups(rows) * r8_quads(cols) * 64; }
 
 // out[m, n] = sum over blocks b of 2^(a's and w's scales of b) times the products' sum, + bias[n]
 struct Rows8ProductArgs {

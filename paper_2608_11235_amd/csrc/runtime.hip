@@ -1177,13 +1177,7 @@ extern "C" cora_status cora_cache_attention(const cora_cache* cache, int32_t lay
   return exception_status();
 }
 
-// The QKV projection leaves fp32 partials in the split-K workspace; the store adds them in split
-// order, rotates, and writes q row-major and K, V into the pages; the attention then uses the same
-// workspace for its key ranges.
-extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cache, const cora_pages* p,
-                                           const cora_chunk* ch, const int32_t* d_tokens, int32_t max_count,
-                                           int32_t max_len, int32_t causal, uint16_t* d_logits,
-                                           void* hip_stream) try {
+static cora_status check_cached_pass(const cora_model* m, const cora_cache* cache, const cora_pages* p, const cora_chunk* ch) {
   if (!m) return fail(CORA_ERR_INVALID_ARG, "null model");
   if (cora_status e = check_cache(cache, 0)) return e;
   if (cora_status e = check_pages(p)) return e;
@@ -1193,43 +1187,90 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
     return fail(CORA_ERR_INVALID_ARG, "the cache's layers, kv heads or head_dim are not the model's");
   if (p->page_size != cache->page_size || p->n_pages != cache->n_pages)
     return fail(CORA_ERR_INVALID_ARG, "cache and pages differ in page_size or n_pages");
-  const int M = ch->rows, d = c.d_model, hd = c.head_dim;
-  if (M == 0) return CORA_OK;  // no row: the arrays may be null
-  if (!d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null tokens or logits");
+  return CORA_OK;
+}
+
+static cora_status check_cached_rows(const cora_model* m, int M) {
   if ((int64_t)M > (int64_t)m->max_batch * m->max_seq || (size_t)M * m->qkv_n > m->splitk_ws_floats)
     return fail(CORA_ERR_UNSUPPORTED, "chunk rows exceed the model's workspace: use several chunks");
+  return CORA_OK;
+}
+
+// What the layers of one cached pass have in common.
+struct CachedPass {
+  const cora_cache* cache;
+  const cora_pages* p;
+  const cora_chunk* ch;
+  CacheAttnPlan plan;
+  int causal;
+  bool beyond;  // positions that the cache has room for and the model's table of angles does not
+};
+
+static cora_status begin_cached_pass(cora_model* m, const CachedPass& x, const int32_t* d_tokens, hipStream_t s) {
+  const auto& c = m->cfg;
+  const int M = x.ch->rows;
+  if (x.beyond)
+    HIP_TRY(launch_rope_rows(x.ch->positions, x.ch->cu + x.p->B, m->rope_cs, m->max_seq_pad, m->rope_freq, M, c.head_dim / 2,
+                             m->rope_rows, s));
+  HIP_TRY(launch_embed(d_tokens, m->embed, m->h, M, c.d_model, c.vocab, m->ones, c.n_layers ? m->a : nullptr, c.rms_eps, s));
+  return CORA_OK;
+}
+
+// Layer l from the projection's `splits` fp32 partials in the split-K workspace to the attention's output in m->attn.
+static cora_status cached_attention(cora_model* m, const CachedPass& x, size_t l, int splits, hipStream_t s) {
+  const auto& c = m->cfg;
+  const int M = x.ch->rows, hd = c.head_dim;
+  const size_t layer_elems = cache_layer_elems(x.cache);
+  CacheStoreArgs st{};
+  st.xf = m->splitk_ws; st.ld = m->qkv_n; st.slab = (int64_t)M * m->qkv_n; st.splits = splits;
+  st.bias = m->layers[l].bqkv;
+  st.rows = M; st.H = c.n_heads; st.Hkv = c.n_kv_heads; st.shift = page_shift(x.cache->page_size);
+  st.n_slots = x.cache->n_pages * x.cache->page_size;
+  st.positions = x.ch->positions; st.slots = x.ch->slots; st.cu_end = x.ch->cu + x.p->B;
+  st.rope = x.beyond ? m->rope_rows : m->rope_cs; st.n_pos = m->max_seq_pad; st.rope_by_row = x.beyond;
+  st.k = x.cache->k + l * layer_elems; st.v = x.cache->v + l * layer_elems; st.q = m->q;
+  HIP_TRY(launch_cache_store(st, hd, true, s));
+  CacheAttnArgs a{};
+  a.q = m->q; a.out = m->attn; a.k = st.k; a.v = st.v;
+  a.table = x.p->table; a.len = x.p->len; a.start = x.ch->start; a.cu = x.ch->cu;
+  a.B = x.p->B; a.rows = M; a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.shift = st.shift;
+  a.n_pages = x.p->n_pages; a.max_pages = x.p->max_pages; a.causal = x.causal ? 1 : 0; a.panels = 1;
+  a.scale_log2 = LOG2E / sqrtf((float)hd);
+  HIP_TRY(launch_cache_attention(a, x.plan, hd, m->splitk_ws, s));
+  return CORA_OK;
+}
+
+static CachedPass cached_pass(const cora_model* m, const cora_cache* cache, const cora_pages* p, const cora_chunk* ch,
+                              int32_t max_count, int32_t max_len, int32_t causal) {
+  const auto& c = m->cfg;
+  const int64_t most = (int64_t)p->max_pages * p->page_size;
+  return CachedPass{cache, p, ch,
+                    cache_attention_plan(p->B, ch->rows, c.n_heads, c.n_kv_heads, c.head_dim, expected(max_count, ch->rows),
+                                         expected(max_len, most), m->num_cus, m->splitk_ws_floats),
+                    causal, most > m->max_seq_pad};
+}
+
+// The QKV projection leaves fp32 partials in the split-K workspace; the store adds them in split
+// order, rotates, and writes q row-major and K, V into the pages; the attention then uses the same
+// workspace for its key ranges.
+extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cache, const cora_pages* p,
+                                           const cora_chunk* ch, const int32_t* d_tokens, int32_t max_count,
+                                           int32_t max_len, int32_t causal, uint16_t* d_logits,
+                                           void* hip_stream) try {
+  if (cora_status e = check_cached_pass(m, cache, p, ch)) return e;
+  const int M = ch->rows, d = m->cfg.d_model;
+  if (M == 0) return CORA_OK;  // no row: the arrays may be null
+  if (!d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null tokens or logits");
+  if (cora_status e = check_cached_rows(m, M)) return e;
   const hipStream_t s = S(hip_stream);
-  const size_t layer_elems = cache_layer_elems(cache);
-  const CacheAttnPlan pl = cache_attention_plan(
-      p->B, M, c.n_heads, c.n_kv_heads, hd, expected(max_count, M),
-      expected(max_len, (int64_t)p->max_pages * p->page_size), m->num_cus, m->splitk_ws_floats);
+  const CachedPass x = cached_pass(m, cache, p, ch, max_count, max_len, causal);
   GemmPlan gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 0, 0.0);
   if ((size_t)gp.splits * M * m->qkv_n > m->splitk_ws_floats) gp = gemm_plan_split(M, m->qkv_n, d, m->num_cus, 1, 0.0);
-  // positions that the cache has room for and the model's table of angles does not
-  const bool beyond = (int64_t)p->max_pages * p->page_size > m->max_seq_pad;
-  if (beyond)
-    HIP_TRY(launch_rope_rows(ch->positions, ch->cu + p->B, m->rope_cs, m->max_seq_pad, m->rope_freq, M, hd / 2,
-                             m->rope_rows, s));
-  HIP_TRY(launch_embed(d_tokens, m->embed, m->h, M, d, c.vocab, m->ones, c.n_layers ? m->a : nullptr, c.rms_eps, s));
+  if (cora_status e = begin_cached_pass(m, x, d_tokens, s)) return e;
   for (size_t l = 0; l < m->layers.size(); ++l) {
     GemmArgs g{m->a, m->layers[l].wqkv, W_BLOCKS, M, m->qkv_n, d, m->splitk_ws, m->qkv_n, nullptr, 1.0f};
     HIP_TRY(launch_gemm(EPI_PART_F32, g, gp, s));
-    CacheStoreArgs st{};
-    st.xf = m->splitk_ws; st.ld = m->qkv_n; st.slab = (int64_t)M * m->qkv_n; st.splits = gp.splits;
-    st.bias = m->layers[l].bqkv;
-    st.rows = M; st.H = c.n_heads; st.Hkv = c.n_kv_heads; st.shift = page_shift(cache->page_size);
-    st.n_slots = cache->n_pages * cache->page_size;
-    st.positions = ch->positions; st.slots = ch->slots; st.cu_end = ch->cu + p->B;
-    st.rope = beyond ? m->rope_rows : m->rope_cs; st.n_pos = m->max_seq_pad; st.rope_by_row = beyond;
-    st.k = cache->k + l * layer_elems; st.v = cache->v + l * layer_elems; st.q = m->q;
-    HIP_TRY(launch_cache_store(st, hd, true, s));
-    CacheAttnArgs a{};
-    a.q = m->q; a.out = m->attn; a.k = st.k; a.v = st.v;
-    a.table = p->table; a.len = p->len; a.start = ch->start; a.cu = ch->cu;
-    a.B = p->B; a.rows = M; a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.shift = st.shift;
-    a.n_pages = p->n_pages; a.max_pages = p->max_pages; a.causal = causal ? 1 : 0; a.panels = 1;
-    a.scale_log2 = LOG2E / sqrtf((float)hd);
-    HIP_TRY(launch_cache_attention(a, pl, hd, m->splitk_ws, s));
+    if (cora_status e = cached_attention(m, x, l, gp.splits, s)) return e;
     if (cora_status e = after_attention(m, l, M, M, s)) return e;
   }
   const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
@@ -1297,8 +1338,8 @@ static cora_status check_rows8(const cora_rows8* x) {
 extern "C" cora_status cora_rows_bytes(int32_t rows, int32_t cols, size_t* data_bytes, size_t* scale_bytes) try {
   if (!data_bytes || !scale_bytes) return fail(CORA_ERR_INVALID_ARG, "null bytes");
   if (cora_status e = check_rows8_sizes(rows, cols)) return e;
-  *data_bytes = (size_t)r8_groups(rows) * r8_blocks(cols) * R8_BLOCK;
-  *scale_bytes = (size_t)r8_groups(rows) * r8_quads(cols) * 64;
+  *data_bytes = r8_data_bytes(rows, cols);
+  *scale_bytes = r8_scale_bytes(rows, cols);
   return CORA_OK;
 } catch (...) {
   return exception_status();
@@ -1312,7 +1353,8 @@ extern "C" cora_status cora_quantize_rows(const void* d_x, int32_t x_f32, int64_
     return fail(CORA_ERR_INVALID_ARG, "x must be given, aligned to its elements, ld >= cols");
   if ((int64_t)out->rows * r8_quads(out->cols) >= 1 << 27)
     return fail(CORA_ERR_UNSUPPORTED, "rows * ceil(cols / 512) must stay below 2^27");
-  HIP_TRY(launch_quantize_rows(QuantizeArgs{d_x, ld, out->rows, out->cols, out->data, out->scale}, x_f32 != 0, S(hip_stream)));
+  HIP_TRY(launch_quantize_rows(QuantizeArgs{d_x, ld, out->rows, out->cols, out->data, out->scale}, x_f32 ? R8_F32 : R8_BF16,
+                               S(hip_stream)));
   return CORA_OK;
 } catch (...) {
   return exception_status();
@@ -1353,6 +1395,140 @@ extern "C" cora_status cora_rows_product(const cora_rows8* a, const cora_rows8* 
   const Rows8ProductArgs g{a->data, a->scale, w->data, w->scale, M, N, a->cols, d_bias, d_out, ld};
   HIP_TRY(launch_rows8_product(g, pl, out_f32 != 0, out_f32 != 0, static_cast<float*>(workspace), S(hip_stream)));
   return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// ---- the cached pass on 8-bit layer weights ------------------------------------------------------
+// A layer's matrices as 8-bit rows, one after another in the caller's memory, data aligned to 256 bytes.
+struct Matrix8 { int rows, cols; };
+static void layer_matrices(const cora_model* m, Matrix8 (&x)[4]) {
+  const int d = m->cfg.d_model;
+  x[0] = {m->qkv_n, d};
+  x[1] = {d, m->hq};
+  x[2] = {2 * m->f_pad, d};
+  x[3] = {d, m->f_pad};
+}
+static size_t matrix8_bytes(const Matrix8& x) { return align_up(r8_data_bytes(x.rows, x.cols)) + align_up(r8_scale_bytes(x.rows, x.cols)); }
+static size_t layer8_bytes(const cora_model* m) {
+  Matrix8 x[4];
+  layer_matrices(m, x);
+  return matrix8_bytes(x[0]) + matrix8_bytes(x[1]) + matrix8_bytes(x[2]) + matrix8_bytes(x[3]);
+}
+static uint8_t* matrix8(const cora_model* m, void* mem, size_t l, int j) {
+  Matrix8 x[4];
+  layer_matrices(m, x);
+  uint8_t* at = static_cast<uint8_t*>(mem) + l * layer8_bytes(m);
+  for (int i = 0; i < j; ++i) at += matrix8_bytes(x[i]);
+  return at;
+}
+
+extern "C" cora_status cora_model_quantized_bytes(cora_model* m, size_t* bytes) try {
+  if (!m || !bytes) return fail(CORA_ERR_INVALID_ARG, "null model or bytes");
+  *bytes = m->layers.size() * layer8_bytes(m);
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+static cora_status check_quantized(const cora_model* m, const void* d_weights, size_t bytes) {
+  if (m->layers.empty()) return CORA_OK;
+  if (!d_weights || (reinterpret_cast<uintptr_t>(d_weights) & 255) != 0 || bytes < m->layers.size() * layer8_bytes(m))
+    return fail(CORA_ERR_INVALID_ARG, "weights missing, not aligned to 256 bytes or smaller than cora_model_quantized_bytes says");
+  return CORA_OK;
+}
+
+extern "C" cora_status cora_model_quantize(cora_model* m, void* d_weights, size_t bytes, void* hip_stream) try {
+  if (!m) return fail(CORA_ERR_INVALID_ARG, "null model");
+  if (cora_status e = check_quantized(m, d_weights, bytes)) return e;
+  Matrix8 x[4];
+  layer_matrices(m, x);
+  for (size_t l = 0; l < m->layers.size(); ++l) {
+    const auto& ly = m->layers[l];
+    const uint16_t* w[4] = {ly.wqkv, ly.wo, ly.wgu, ly.wd};
+    for (int j = 0; j < 4; ++j) {
+      uint8_t* at = matrix8(m, d_weights, l, j);
+      HIP_TRY(launch_quantize_rows(QuantizeArgs{w[j], 0, x[j].rows, x[j].cols, at, at + align_up(r8_data_bytes(x[j].rows, x[j].cols))},
+                                   R8_BLOCKS, S(hip_stream)));
+    }
+  }
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+// Workspace of a pass of M rows: the widest activations in 8 bits, gate and up in bf16, the products' partial sums.
+struct Quantized8 {
+  size_t data, scale, gate_up, parts, bytes;  // offsets, and all
+};
+static Quantized8 quantized_workspace(const cora_model* m, int M) {
+  const int widest = std::max({m->cfg.d_model, m->hq, m->f_pad});
+  Matrix8 x[4];
+  layer_matrices(m, x);
+  size_t parts = 0;
+  for (const Matrix8& w : x) parts = std::max(parts, rows8_plan(M, w.rows, w.cols, false, m->num_cus).ws_floats * 4);
+  Quantized8 q{};
+  q.scale = align_up(r8_data_bytes(M, widest));
+  q.gate_up = q.scale + align_up(r8_scale_bytes(M, widest));
+  q.parts = q.gate_up + align_up((size_t)M * 2 * m->f_pad * 2);
+  q.bytes = q.parts + align_up(parts);
+  return q;
+}
+
+extern "C" cora_status cora_forward_quantized_workspace(cora_model* m, int32_t rows, size_t* bytes) try {
+  if (!m || !bytes) return fail(CORA_ERR_INVALID_ARG, "null model or bytes");
+  if (rows < 0) return fail(CORA_ERR_INVALID_ARG, "rows >= 0");
+  if (cora_status e = check_cached_rows(m, rows)) return e;
+  *bytes = rows ? quantized_workspace(m, rows).bytes : 0;
+  return CORA_OK;
+} catch (...) {
+  return exception_status();
+}
+
+extern "C" cora_status cora_forward_quantized(cora_model* m, const void* d_weights, size_t weights_bytes,
+                                              const cora_cache* cache, const cora_pages* p, const cora_chunk* ch,
+                                              const int32_t* d_tokens, int32_t max_count, int32_t max_len,
+                                              int32_t causal, uint16_t* d_logits, void* workspace,
+                                              size_t workspace_bytes, void* hip_stream) try {
+  if (cora_status e = check_cached_pass(m, cache, p, ch)) return e;
+  if (cora_status e = check_quantized(m, d_weights, weights_bytes)) return e;
+  const int M = ch->rows, d = m->cfg.d_model;
+  if (M == 0) return CORA_OK;  // no row: the arrays may be null
+  if (!d_tokens || !d_logits) return fail(CORA_ERR_INVALID_ARG, "null tokens or logits");
+  if (cora_status e = check_cached_rows(m, M)) return e;
+  if ((size_t)M * d > m->splitk_ws_floats)
+    return fail(CORA_ERR_UNSUPPORTED, "chunk rows exceed the model's workspace: use several chunks");
+  const Quantized8 q = quantized_workspace(m, M);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < q.bytes)
+    return fail(CORA_ERR_INVALID_ARG, "workspace missing, not aligned to 256 bytes or smaller than cora_forward_quantized_workspace says");
+  const hipStream_t s = S(hip_stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  uint16_t* gate_up = reinterpret_cast<uint16_t*>(ws + q.gate_up);
+  const CachedPass x = cached_pass(m, cache, p, ch, max_count, max_len, causal);
+  Matrix8 dims[4];
+  layer_matrices(m, dims);
+  // out = the 8-bit rows of `from` times matrix j of layer l, in fp32 (sums of the 8-bit instruction) or bf16
+  auto product = [&](size_t l, int j, const void* from, int64_t ld, R8Source how, void* out, bool f32) -> cora_status {
+    const Matrix8& w = dims[j];
+    const uint8_t* at = matrix8(m, const_cast<void*>(d_weights), l, j);
+    HIP_TRY(launch_quantize_rows(QuantizeArgs{from, ld, M, w.cols, ws + q.data, ws + q.scale}, how, s));
+    const Rows8ProductArgs g{ws + q.data, ws + q.scale, at, at + align_up(r8_data_bytes(w.rows, w.cols)), M, w.rows, w.cols, nullptr, out, w.rows};
+    HIP_TRY(launch_rows8_product(g, rows8_plan(M, w.rows, w.cols, false, m->num_cus), f32, false, reinterpret_cast<float*>(ws + q.parts), s));
+    return CORA_OK;
+  };
+  if (cora_status e = begin_cached_pass(m, x, d_tokens, s)) return e;
+  for (size_t l = 0; l < m->layers.size(); ++l) {
+    if (cora_status e = product(l, 0, m->a, 0, R8_PANELS, m->splitk_ws, true)) return e;
+    if (cora_status e = cached_attention(m, x, l, 1, s)) return e;
+    if (cora_status e = product(l, 1, m->attn, 0, R8_PANELS, m->splitk_ws, true)) return e;
+    HIP_TRY(launch_residual_norm(m->h, m->splitk_ws, 1, M, d, m->ones, m->a, m->cfg.rms_eps, s));
+    if (cora_status e = product(l, 2, m->a, 0, R8_PANELS, gate_up, false)) return e;
+    if (cora_status e = product(l, 3, gate_up, 2 * m->f_pad, R8_SWIGLU, m->splitk_ws, true)) return e;
+    // the last layer's output is normalised by the LM head
+    HIP_TRY(launch_residual_norm(m->h, m->splitk_ws, 1, M, d, m->ones, l + 1 < m->layers.size() ? m->a : nullptr, m->cfg.rms_eps, s));
+  }
+  const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
+  return lm_head(m, all, M, M, d_logits, s);
 } catch (...) {
   return exception_status();
 }

@@ -1,0 +1,232 @@
+"""Cached passes whose layers' products are in 8 bits: against the same pass in 64 bits, rounded where it rounds."""
+import numpy as np
+import pytest
+import torch
+
+import seeded_inputs as si
+from oracle import forward as of
+from paper_2608_11235_amd import Chunk, KVCache, Model, cache_plan, cache_reorder, vocab_beam
+from paper_2608_11235_amd._lib import CoraError
+from tests.gpu_common import log_case, require_gpu
+from tests.rows8_ref import quantized
+from tests.test_gpu_cached_pass import HD128, cache_for, masked_logits, put
+
+pytestmark = pytest.mark.gpu
+
+WIDE = si.ModelSpec("wide8", 2, 512, 8, 2, 128, 1376, 900, 5, True, 1e-6, 1e6, 4.0)
+MODELS = {"tiny": si.TINY, "hd128": HD128, "wide": WIDE}
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).double().numpy()
+
+
+def eight(x):
+    v, e = quantized(torch.from_numpy(np.ascontiguousarray(x)))
+    return (v.view(len(x), -1, 128) * torch.exp2(e.double())[..., None]).view(len(x), -1)[:, :x.shape[1]].numpy()
+
+
+def quantized_logits(w, spec, tokens, seen):
+    """masked_logits with the four products of a layer on 8-bit operands and bf16 where the pass stores bf16."""
+    L, H, Hkv, hd = len(tokens), spec.n_heads, spec.n_kv_heads, spec.head_dim
+    cos, sin = of.rope_tables(L, hd, spec.rope_theta)
+    h = np.asarray(w.embed_rows(tokens), np.float64)
+    for i in range(spec.n_layers):
+        p = {k: np.asarray(v, np.float64) for k, v in w.layer(i).items() if v is not None}
+        a = eight(bf16(of.rmsnorm(h, p["attn_norm"], spec.rms_eps)))
+        q, k, v = a @ eight(p["wq"]).T, a @ eight(p["wk"]).T, a @ eight(p["wv"]).T
+        if spec.qkv_bias:
+            q, k, v = q + p["bq"], k + p["bk"], v + p["bv"]
+        q = bf16(of.rope(q.reshape(L, H, hd).transpose(1, 0, 2), cos, sin))
+        k = bf16(of.rope(k.reshape(L, Hkv, hd).transpose(1, 0, 2), cos, sin))
+        v = bf16(v.reshape(L, Hkv, hd).transpose(1, 0, 2))
+        o = np.empty((L, H, hd))
+        for j in range(H):
+            s = q[j] @ k[j * Hkv // H].T / np.sqrt(hd)
+            o[:, j] = of.softmax(np.where(seen, s, -np.inf)) @ v[j * Hkv // H]
+        h = h + eight(bf16(o.reshape(L, H * hd))) @ eight(p["wo"]).T
+        a = eight(bf16(of.rmsnorm(h, p["mlp_norm"], spec.rms_eps)))
+        u = of.silu(bf16(a @ eight(p["wg"]).T)) * bf16(a @ eight(p["wu"]).T)
+        h = h + eight(u) @ eight(p["wd"]).T
+    return of.logits_from_hidden(w, spec, h)
+
+
+def values(bits):
+    return bits.view(torch.bfloat16).double().cpu().numpy()
+
+
+@pytest.mark.parametrize("name", MODELS)
+@pytest.mark.parametrize("lens,rows", [([70, 1, 33], 120), ([5, 20, 1], 30), ([150, 90, 130], 370)])
+def test_pass_against_64_bits(name, lens, rows):
+    """What the pass is off, in units of what 8 bits change (a rounding to steps changes a number by 12^-1/2 = 0.29 steps,
+    root mean square).  Numbers that differ by d steps before it differ by one step in d of the cases, d^1/2 steps.
+    The kernel rounds the attention's terms to bf16, which the definition does not: 2^-9 or 0.015 steps, 0.12 steps of
+    0.29, 0.4 times what 8 bits change there, and once the next layer's rows differ by that much, 2 % or 0.16 steps, 0.4
+    steps: more than 0.29.  The mean square over two layers' eight products, (0 + 0.4^2 + 2 * 0.25^2 + 4 * 1.0^2) / 8, is
+    0.74^2."""
+    require_gpu()
+    spec = MODELS[name]
+    log_case(f"quantized pass {name} {lens}")
+    rng = np.random.default_rng(rows)
+    cache, chunk = cache_for(spec, 3, max(lens) + 8), Chunk(3, rows)
+    put(chunk.count, lens)
+    cache_plan(cache, chunk)
+    tokens = rng.integers(0, spec.vocab, size=rows)
+    w = si.HostWeights(spec, 0)
+    with Model(spec, 0, 4, 128) as m:
+        w8 = m.quantize()
+        tok = torch.as_tensor(tokens.astype(np.int32)).cuda()
+        got = values(m.forward_cached(cache, chunk, tok, causal=True, weights=w8))
+        again = values(m.forward_cached(cache, chunk, tok, causal=True, weights=w8))
+        assert np.array_equal(got[:sum(lens)], again[:sum(lens)])
+    at = 0
+    for n in lens:
+        seen = np.tril(np.ones((n, n), bool))
+        want = quantized_logits(w, spec, tokens[at:at + n], seen)
+        full = masked_logits(w, spec, tokens[at:at + n], seen)
+        off, change = np.linalg.norm(got[at:at + n] - want), np.linalg.norm(want - full)
+        log_case(f"  {n} rows: off {off / np.linalg.norm(want):.4f}, 8 bits change {change / np.linalg.norm(full):.4f}")
+        assert off <= 0.75 * change
+        at += n
+
+
+@pytest.mark.parametrize("d,ffn,bias", [(256, 300, False), (512, 1376, True), (1024, 512, True)])
+@pytest.mark.parametrize("rows", [30, 64, 120, 370])
+def test_one_layer_of_single_rows(d, ffn, bias, rows):
+    """Requests of one key: the attention's output is v itself, and fp32 sums, off by 5e-5 at the most, move a bf16 number
+    in 1 % of the cases and the 8-bit number behind it in 3 % of these: less than one of a row's 4000, and one of 1000
+    numbers that moves by a step is a tenth of what 8 bits change in a product.  The logits' own rounding is 2^-9 of them,
+    0.03 of the 0.07 that 8 bits change.  Half the rows stay below 0.15."""
+    require_gpu()
+    spec = si.ModelSpec("one", 1, d, 8, 2, 128, ffn, 900, 5, bias, 1e-6, 1e6, 4.0)
+    log_case(f"quantized layer d={d} ffn={ffn} rows={rows}")
+    cache, chunk = cache_for(spec, rows, 8), Chunk(rows, rows)
+    put(chunk.count, [1] * rows)
+    cache_plan(cache, chunk)
+    tokens = np.random.default_rng(rows).integers(0, spec.vocab, size=rows)
+    w, one = si.HostWeights(spec, 0), np.ones((1, 1), bool)
+    with Model(spec, 0, 4, 128) as m:
+        got = values(m.forward_cached(cache, chunk, torch.as_tensor(tokens.astype(np.int32)).cuda(), causal=True, weights=m.quantize()))
+    ratio = []
+    for i in list(range(8)) + list(range(rows - 7, rows)):
+        want, full = quantized_logits(w, spec, tokens[i:i + 1], one), masked_logits(w, spec, tokens[i:i + 1], one)
+        ratio.append(np.linalg.norm(got[i:i + 1] - want) / np.linalg.norm(want - full))
+    log_case(f"  {np.round(sorted(ratio), 3)}")
+    assert np.median(ratio) <= 0.15 and max(ratio) <= 0.75
+
+
+def test_steps_read_what_chunks_stored():
+    """A prompt, then a token at a time: the logits of one chunk of all, off by what other splits of the attention's keys
+    lead to (as above); and the two passes read one cache."""
+    require_gpu()
+    log_case("quantized steps")
+    spec = HD128
+    rng = np.random.default_rng(2)
+    tokens = rng.integers(0, spec.vocab, size=(2, 40)).astype(np.int32)
+    with Model(spec, 0, 2, 64) as m:
+        w8 = m.quantize()
+
+        def whole(weights):
+            cache, chunk = cache_for(spec, 2, 64), Chunk(2, 80)
+            put(chunk.count, [40, 40])
+            cache_plan(cache, chunk)
+            return values(m.forward_cached(cache, chunk, torch.as_tensor(tokens.reshape(-1)).cuda(), causal=True, weights=weights)).reshape(2, 40, -1)
+
+        want, full = whole(w8), whole(None)
+        cache, first, step = cache_for(spec, 2, 64), Chunk(2, 60), Chunk(2, 2)
+        put(first.count, [30, 30])
+        cache_plan(cache, first)
+        m.forward_cached(cache, first, torch.as_tensor(np.ascontiguousarray(tokens[:, :30]).reshape(-1)).cuda(), causal=True, weights=w8)
+        step.count.fill_(1)
+        for t in range(30, 40):
+            step.start.copy_(cache.len)
+            cache_plan(cache, step)
+            got = values(m.forward_cached(cache, step, torch.as_tensor(np.ascontiguousarray(tokens[:, t])).cuda(), causal=True, weights=w8))
+            assert np.linalg.norm(got - want[:, t]) <= 0.75 * np.linalg.norm(want[:, t] - full[:, t])
+        mixed = values(m.forward_cached(cache, step, torch.as_tensor(np.ascontiguousarray(tokens[:, 39])).cuda(), causal=True))
+        assert np.linalg.norm(mixed - full[:, 39]) <= np.linalg.norm(want[:, 39] - full[:, 39])
+
+
+def test_beams_on_8_bit_weights():
+    """A captured step of plan, 8-bit pass, choice and reorder, replayed: what eager calls give."""
+    require_gpu()
+    log_case("quantized beams")
+    spec, K = HD128, 3
+    rng = np.random.default_rng(4)
+
+    def start(m, w8):
+        cache = KVCache(spec.n_layers, 40, spec.n_kv_heads, spec.head_dim, 32, 2 * K, 6, shared=True)
+        first = Chunk(2 * K, 64)
+        put(first.count, [33, 0, 0, 20, 0, 0])
+        cache_plan(cache, first)
+        tok = torch.as_tensor(np.random.default_rng(9).integers(0, spec.vocab, 64).astype(np.int32)).cuda()
+        m.forward_cached(cache, first, tok, causal=True, weights=w8)
+        cache_reorder(cache, torch.tensor([0, 0, 0, 3, 3, 3], dtype=torch.int32, device="cuda"))
+        return cache
+
+    with Model(spec, 0, 2, 64) as m:
+        w8 = m.quantize()
+        runs = []
+        for captured in (False, True):
+            cache, chunk = start(m, w8), Chunk(2 * K, 2 * K)
+            chunk.count.fill_(1)
+            token = torch.tensor([5, 6, 7, 8, 9, 10], dtype=torch.int32, device="cuda")
+            score = torch.tensor([0.0, -1.0, -2.0] * 2, device="cuda")
+            ws = torch.empty(m.quantized_workspace(2 * K), dtype=torch.uint8, device="cuda")
+            parent = torch.zeros(2 * K, dtype=torch.int32, device="cuda")
+
+            def step():
+                chunk.start.copy_(cache.len)
+                cache_plan(cache, chunk)
+                logits = m.forward_cached(cache, chunk, token, max_count=1, max_len=192, causal=True, weights=w8, workspace=ws)
+                tok, par, nxt = vocab_beam(logits, K, spec.mask_id, score)
+                token.copy_(tok.view(-1))
+                parent.copy_(par.view(-1))
+                score.copy_(nxt.view(-1))
+                cache_reorder(cache, parent)
+
+            history = []
+            if captured:
+                side = torch.cuda.Stream()
+                keep = [t.clone() for t in (token, score, parent, cache.table, cache.len, cache.refs, cache.free, cache.n_free, cache.k, cache.v)]
+                side.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(side):
+                    step()
+                torch.cuda.synchronize()
+                for t, old in zip((token, score, parent, cache.table, cache.len, cache.refs, cache.free, cache.n_free, cache.k, cache.v), keep):
+                    t.copy_(old)
+                g = torch.cuda.CUDAGraph()
+                torch.cuda.synchronize()
+                with torch.cuda.graph(g):
+                    step()
+            for _ in range(8):
+                g.replay() if captured else step()
+                torch.cuda.synchronize()
+                history.append((token.tolist(), parent.tolist(), score.tolist(), cache.len.tolist(), cache.refs.tolist()))
+            runs.append(history)
+        assert runs[0] == runs[1]
+        assert all(len(set(p)) >= 2 for _, p, *_ in runs[0])
+
+
+def test_refusals():
+    require_gpu()
+    spec = si.TINY
+    cache, chunk = cache_for(spec, 1, 64), Chunk(1, 16)
+    put(chunk.count, [16])
+    cache_plan(cache, chunk)
+    tok = torch.zeros(16, dtype=torch.int32, device="cuda")
+    with Model(spec, 0, 1, 64) as m:
+        w8 = m.quantize()
+        with pytest.raises(CoraError, match="weights"):
+            m.forward_cached(cache, chunk, tok, weights=w8[:-1])
+        with pytest.raises(CoraError, match="workspace"):
+            m.forward_cached(cache, chunk, tok, weights=w8, workspace=torch.empty(m.quantized_workspace(16) - 1, dtype=torch.uint8, device="cuda"))
+        with pytest.raises(ValueError, match="out"):
+            m.quantize(out=w8[:-1])
+        with pytest.raises(TypeError, match="weights"):
+            m.forward_cached(cache, chunk, tok, weights=w8.view(torch.int8))
+        with pytest.raises(CoraError, match="workspace"):
+            m.quantized_workspace(65)
+        empty = Chunk(1, 0)
+        assert m.forward_cached(cache, empty, tok[:0], weights=w8).shape == (0, spec.vocab)
+        m.forward_cached(cache, chunk, tok, weights=w8)
