@@ -22,6 +22,7 @@ constexpr int BT = 256;         // threads of a range
 constexpr int BE = 16;          // logits of a thread and tile
 constexpr int TILE = BT * BE;
 constexpr int CAP = 512;       // held candidates of a range
+constexpr int RANK = 8;          // compared at a time
 constexpr float LOWEST = -3.3895313892515355e38f;  // bf16's lowest finite number
 // LOG2E's own error, relative: a sum of 2^(v LOG2E) is that of exp(v (1 + this)), which for the terms that count,
 // those near the largest, is a factor 1 + this times v
@@ -40,10 +41,10 @@ __device__ __forceinline__ uint64_t candidate(uint32_t o, int id) { return (uint
 __device__ __forceinline__ int id_of(uint64_t c) { return (int)(0xffffffffu - (uint32_t)c); }
 
 // The W largest of list[0 .. n) in falling order at its front; their number.  The list's rest is undefined; it has
-// room for four more.  Four are compared at a time (one after the other, each waits for its own load from LDS).
+// room for RANK more.  RANK are compared at a time (one after the other, each waits for its own load from LDS).
 __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t* least) {
   const int tid = threadIdx.x;
-  if (tid < 4) list[n + tid] = 0;
+  if (tid < RANK) list[n + tid] = 0;
   __syncthreads();
   uint64_t own[CAP / BT];
   int rank[CAP / BT];
@@ -54,12 +55,12 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
     if (tid + e * BT < n) {
       own[e] = list[tid + e * BT];
       int r = 0;
-      for (int i = 0; i < n; i += 4) {
-        uint64_t x[4];
+      for (int i = 0; i < n; i += RANK) {
+        uint64_t x[RANK];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = list[i + u];
+        for (int u = 0; u < RANK; ++u) x[u] = list[i + u];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) r += x[u] > own[e] ? 1 : 0;
+        for (int u = 0; u < RANK; ++u) r += x[u] > own[e] ? 1 : 0;
       }
       rank[e] = r;
     }
@@ -77,12 +78,13 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 
 }  // namespace
 
-// Bound by its instructions, eight a logit, of them one exponential: 1024 x 152064 in 72 us (4.3 TB/s) with four workgroups of
-// 256 threads a CU (two of 512: 80; a second tile ahead: 76; 32 logits a thread: 105, in scratch memory).
+// 1024 x 152064 in 70 us (4.4 TB/s) with four workgroups of 256 threads a CU: without the candidates 59, without the exponentials 63,
+// without both 57.  Slower were two workgroups of 512 (80), 32 logits a thread (105, in scratch memory), lists of the wavefronts' own
+// in place of the workgroup's barriers (94: four times the candidates) and a cut at 64 or 128 held candidates (72, 79).
 // Of a row's logits those in whole 16-byte blocks are loaded eight at a time, a tile ahead; the up to seven on either
 // side are one each of the first threads', before the first tile.
 __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
-  __shared__ __attribute__((aligned(16))) uint64_t list[CAP + 4];
+  __shared__ __attribute__((aligned(16))) uint64_t list[CAP + RANK];
   __shared__ uint64_t least;      // candidates below it are out
   __shared__ int held;
   __shared__ uint64_t group_best[64];  // of BT / 64 threads each
@@ -92,7 +94,7 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   const int part = blockIdx.x % a.parts;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;  // no candidates, or the one without logits
-  const int W = a.W, trim = max(64, 4 * W);  // held candidates beyond which they are cut down to the W best
+  const int W = a.W, trim = max(32, 2 * W);  // held candidates beyond which they are cut down to the W best
   const uint16_t* x = a.logits + row * a.ld;
   const int head = min(a.V, (int)(-((uintptr_t)x >> 1) & 7)), blocks = (a.V - head) / 8;
   const int b0 = min(part * a.chunk, blocks), b1 = min(b0 + a.chunk, blocks);  // blocks of this range
@@ -279,30 +281,33 @@ __device__ __forceinline__ double score_of(key_t k) {
   return __builtin_bit_cast(double, k[0] >> 63 ? k[0] ^ 1ull << 63 : ~k[0]);
 }
 __device__ __forceinline__ bool before(key_t x, key_t y) { return x[0] > y[0] || (x[0] == y[0] && x[1] > y[1]); }
-// how many of n keys come before one; the list has room for four more, which are none
+// how many of n keys come before that of four lanes, which go over a quarter each; the list has room for 4 RANK more,
+// which are none
 __device__ __forceinline__ int rank_of(const key_t* keys, int n, key_t mine) {
   int r = 0;
-  for (int i = 0; i < n; i += 4) {
-    key_t x[4];
+  for (int i = threadIdx.x & 3; i < n; i += 4 * RANK) {
+    key_t x[RANK];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = keys[i + u];
+    for (int u = 0; u < RANK; ++u) x[u] = keys[i + 4 * u];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) r += before(x[u], mine) ? 1 : 0;
+    for (int u = 0; u < RANK; ++u) r += before(x[u], mine) ? 1 : 0;
   }
-  return r;
+  r += __shfl_xor(r, 1, 64);
+  return r + __shfl_xor(r, 2, 64);
 }
 
 }  // namespace
 
 static_assert(BEAM_MAX <= 64, "a beam's number in six bits above a candidate's 48");
 
-// Bound by latency: loads of the ranges' numbers, a logarithm a beam, and ranks by comparing all with all.
+// Bound by latency: the ranges' numbers, a logarithm a beam, and ranks by comparing all with all, four lanes a candidate.
+// 128 requests of 8 x 16 candidates 5.3 us (a lane a candidate: 6.8).
 __global__ __launch_bounds__(512) void k_beam_merge(BeamArgs a) {
   extern __shared__ __attribute__((aligned(16))) char mem[];
   const int tid = threadIdx.x, K = a.K, P = a.parts, W = a.W, lists = K * P;
   const int64_t row0 = (int64_t)blockIdx.x * K;
-  key_t* keys = reinterpret_cast<key_t*>(mem);          // [max(W W, lists) + 4]
-  double* base = reinterpret_cast<double*>(keys + max(W * W, lists) + 4);  // [K] score minus the log of the row's sum; NaN: no candidate
+  key_t* keys = reinterpret_cast<key_t*>(mem);          // [max(W W, lists) + 4 RANK]
+  double* base = reinterpret_cast<double*>(keys + max(W * W, lists) + 4 * RANK);  // [K] score minus the log of the row's sum; NaN: no candidate
   double* origin = base + K;                            // [K] which is relative to this (logits of 1e38 keep the score's bits)
   __shared__ int n_in;
   __shared__ key_t least;
@@ -311,41 +316,54 @@ __global__ __launch_bounds__(512) void k_beam_merge(BeamArgs a) {
     least = key_t{0, 0};
   }
   auto is_done = [&](int k) { return a.done && a.done[row0 + k]; };
-  for (int k = tid; k < K; k += 512) {
+  // the first candidate of a thread is on its way while the sums are made
+  const uint64_t early = tid < lists * W ? a.best[row0 * P * W + tid] : 0;
+  for (int k = tid >> 6; k < K; k += 8) {  // a wavefront a beam
+    const int lane = tid & 63;
     const double s = a.score[row0 + k];
-    double b = __builtin_nan(""), top = 0;
+    double b = __builtin_nan(""), top = -INFINITY, sum = 0;
     if (s > -INFINITY && s < INFINITY) {
       if (is_done(k)) {
         b = s;
+        top = 0;
       } else {
         const double* st = a.stats + 2 * (row0 + k) * P;
-        double sum = 0;
-        top = st[0];
-        for (int p = 1; p < P; ++p) top = fmax(top, st[2 * p]);
-        for (int p = 0; p < P; ++p) sum += st[2 * p + 1] * exp(st[2 * p] - top);
+        for (int p = lane; p < P; p += 64) {
+          const double t = st[2 * p], u = st[2 * p + 1], was = top;
+          top = fmax(top, t);
+          sum = sum * exp(was - top) + u * exp(t - top);
+        }
+        double all = top;
+        for (int d = 1; d < min(P, 64); d <<= 1) all = fmax(all, __shfl_xor(all, d, 64));
+        if (P > 1) sum *= exp(top - all);
+        for (int d = 1; d < min(P, 64); d <<= 1) sum += __shfl_xor(sum, d, 64);
+        top = all;
         if (sum > 0 && sum < INFINITY) b = s - log(sum);
       }
     }
-    base[k] = b;
-    origin[k] = top;
+    if (lane == 0) {
+      base[k] = b;
+      origin[k] = top;
+    }
   }
   __syncthreads();
   // candidate i of list l (a beam's range), in the list's falling order
   auto get = [&](int l, int i) {
-    const int k = l / P;
+    const int k = l / P, c = l * W + i;
     const double b = base[k];
     if (!(b == b)) return key_t{0, 0};
     if (is_done(k)) return l % P == 0 && i == 0 ? key_of(b, k, 1) : key_t{0, 0};
-    const uint64_t w = a.best[((row0 + k) * P + l % P) * W + i];
+    const uint64_t w = c == tid ? early : a.best[row0 * P * W + c];
     return w ? key_of(b + ((double)of_ordered((uint32_t)(w >> 32)) - origin[k]), k, w) : key_t{0, 0};
   };
   // the W'th of the lists' heads: a candidate behind it has that many others before it
   if (lists > W) {
-    for (int l = tid; l < lists + 4; l += 512) keys[l] = l < lists ? get(l, 0) : key_t{0, 0};
+    for (int l = tid; l < lists + 4 * RANK; l += 512) keys[l] = l < lists ? get(l, 0) : key_t{0, 0};
     __syncthreads();
-    for (int l = tid; l < lists; l += 512) {
+    for (int l = tid >> 2; l < lists; l += 128) {
       const key_t mine = keys[l];
-      if (mine[0] && rank_of(keys, lists, mine) == W - 1) least = mine;
+      const int rank = rank_of(keys, lists, mine);
+      if (mine[0] && rank == W - 1) least = mine;
     }
     __syncthreads();
   }
@@ -357,13 +375,13 @@ __global__ __launch_bounds__(512) void k_beam_merge(BeamArgs a) {
   }
   __syncthreads();
   const int n = n_in;
-  if (tid < 4) keys[n + tid] = key_t{0, 0};
+  if (tid < 4 * RANK) keys[n + tid] = key_t{0, 0};
   __syncthreads();
   const int64_t out = (int64_t)blockIdx.x * W;
-  for (int c = tid; c < n; c += 512) {
+  for (int c = tid >> 2; c < n; c += 128) {
     const key_t mine = keys[c];
     const int rank = rank_of(keys, n, mine), k = 63 - (int)(mine[1] >> 48);
-    if (rank < W) {
+    if (rank < W && (tid & 3) == 0) {
       a.token[out + rank] = is_done(k) ? a.done_token : id_of(mine[1]);
       a.parent[out + rank] = (int)(row0 + k);
       a.next[out + rank] = (float)score_of(mine);
@@ -395,7 +413,7 @@ hipError_t launch_vocab_beam(BeamArgs a, const BeamPlan& p, void* ws, hipStream_
   a.best = reinterpret_cast<uint64_t*>(a.stats + 2 * (size_t)a.B * a.K * a.parts);
   hipLaunchKernelGGL(k_beam_rows, dim3((unsigned)((int64_t)a.B * a.K * a.parts)), dim3(BT), 0, s, a);
   if (hipError_t e = hipGetLastError()) return e;
-  const size_t lds = 16 * ((size_t)std::max(a.W * a.W, a.K * a.parts) + 4 + a.K);
+  const size_t lds = 16 * ((size_t)std::max(a.W * a.W, a.K * a.parts) + 4 * RANK + a.K);
   hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.B), dim3(512), lds, s, a);
   return hipGetLastError();
 }
