@@ -88,34 +88,49 @@ __device__ __forceinline__ void settled_barrier() {
   __syncthreads();
 }
 
+// A thread's first page entry (i = threadIdx.x) where its request lets go of it: the page, or -1; the
+// request; the count before.
+struct LetGo {
+  int page = -1, b = 0, was = 0;
+};
+
 // Page entries [0, total) of the requests (entry i belongs to the last b with first[b] <= i) that their
 // requests let go of; refs has been lowered.  Those that nobody holds go onto the stack in the order of
-// the entries, each from its lowest request, which the others learn through the count itself: below
-// zero it is INT_MIN + that request.  Returns their number.
+// the entries, each from its lowest request.  Up to PT entries of which none shares such a page need no
+// more than the counts, before (1) and now (0); else the requests learn through the count itself which is
+// the lowest: below zero it is INT_MIN + that request.  Returns the pages' number.
 template <class Drops>
 __device__ __forceinline__ int push_unheld(const int32_t* table, int32_t* refs, int32_t* free, int B, int max_pages, int n_pages,
-                                           int n_free, const uint32_t* first, uint32_t total, Drops&& drops,
+                                           int n_free, const uint32_t* first, uint32_t total, Drops&& drops, LetGo own,
                                            uint32_t (*part)[PT / 64]) {
   auto entry = [&](uint32_t i, int& b) {
+    if (i == threadIdx.x) {
+      b = own.b;
+      return own.page;
+    }
     b = owner(first, B, i);
     if (!drops(b)) return -1;
     const int page = table[(int64_t)b * max_pages + (i - first[b])];
     return (uint32_t)page < (uint32_t)n_pages ? page : -1;
   };
   settled_barrier();
-  for (uint32_t i = threadIdx.x; i < total; i += PT) {
-    int b;
-    const int page = entry(i, b);
-    if (page >= 0 && count_of(refs, page) <= 0) atomicMin(refs + page, INT_MIN + b);
+  const int now = own.page >= 0 ? count_of(refs, own.page) : 1;
+  const bool together = __syncthreads_or(now <= 0 && own.was != 1) || total > PT;
+  if (together) {
+    for (uint32_t i = threadIdx.x; i < total; i += PT) {
+      int b;
+      const int page = entry(i, b);
+      if (page >= 0 && count_of(refs, page) <= 0) atomicMin(refs + page, INT_MIN + b);
+    }
+    settled_barrier();
   }
-  settled_barrier();
   uint32_t carry[2] = {0, 0};
   const uint32_t room = (uint32_t)(n_pages - n_free);
   for (uint32_t i0 = 0; i0 < total; i0 += PT) {
     const uint32_t i = i0 + threadIdx.x;
     int b = 0;
     const int page = i < total ? entry(i, b) : -1;
-    const bool gives = page >= 0 && count_of(refs, page) == INT_MIN + b;
+    const bool gives = together ? page >= 0 && count_of(refs, page) == INT_MIN + b : now <= 0;
     uint32_t v[2] = {gives ? 1u : 0u, 0};
     block_scan(v, carry, part);
     if (gives) {
@@ -202,12 +217,15 @@ __global__ __launch_bounds__(PT) void k_cache_plan(CachePlanArgs a) {
     if (tid == 0) first_page[B] = back[0];
     __syncthreads();  // first_page is whole
     if constexpr (REFS) {
+      LetGo own;
       for (uint32_t i = tid; i < back[0]; i += PT) {
         const int b = owner(first_page, B, i), page = a.table[(int64_t)b * a.max_pages + (i - first_page[b])];
-        if ((uint32_t)page < (uint32_t)a.n_pages) atomicSub(a.refs + page, 1);
+        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+        const int was = atomicSub(a.refs + page, 1);
+        if (i == (uint32_t)tid) own = {page, b, was};
       }
       n_free += push_unheld(a.table, a.refs, a.free, B, a.max_pages, a.n_pages, n_free, first_page, back[0],
-                            [&](int) { return true; }, part);
+                            [&](int) { return true; }, own, part);
     } else {
     const uint32_t given = min(back[0], (uint32_t)(a.n_pages - n_free));  // more only if a table holds a page twice
     for (uint32_t i = 4 * tid; i < given; i += 4 * PT) {
@@ -346,8 +364,10 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
   int* length = eldest + B;                                // before the call
   int* fresh = length + B;                                 // page of the copy a request gets, or -1
   __shared__ uint32_t part[2][PT / 64];
+  __shared__ int longest;                                  // request's pages
   const int most = a.max_pages << a.shift;
   const int n_free0 = min(max(a.n_free[0], 0), a.n_pages);
+  if (tid == 0) longest = 0;
   for (int b = tid; b < B; b += PT) {
     const int p = a.parent[b];
     const bool valid = p >= -1 && p < B;
@@ -365,11 +385,10 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
       atomicMin(&eldest[parent[b]], b);
     }
   uint32_t carry[2] = {0, 0};
-  int longest = 0;
   for (int b0 = 0; b0 < B; b0 += PT) {
     const int b = b0 + tid;
     const int held = b < B ? pages_of(length[b], a.shift) : 0;
-    longest = max(longest, held);
+    if (held > 0) atomicMax(&longest, held);
     uint32_t v[2] = {(uint32_t)held, 0};
     block_scan(v, carry, part);
     if (b < B) first[b] = v[0] - (uint32_t)held;
@@ -378,8 +397,29 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
   if (tid == 0) first[B] = total;
   __syncthreads();
 
+  // The tables change last, PT RE entries at a time; what the first of them hold is on its way until then.
+  const int cols = max(1, min(longest, PT * RE / B)), n = B * cols;
+  int value[RE];
+  auto read = [&](int c0) {
+#pragma unroll
+    for (int u = 0; u < RE; ++u) {
+      value[u] = 0;
+      const int e = tid + u * PT;
+      if (e >= n) continue;
+      const int p = parent[e / cols], col = c0 + e % cols;
+      if (p >= 0 && col < pages_of(length[p], a.shift)) value[u] = a.table[(int64_t)p * a.max_pages + col];
+    }
+  };
+  read(0);
+  auto last_page = [&](int b) {  // of its parent
+    const int p = parent[b];
+    return p >= 0 && length[p] >> a.shift < a.max_pages ? a.table[(int64_t)p * a.max_pages + (length[p] >> a.shift)] : -1;
+  };
+  const int own_last = tid < B ? last_page(tid) : -1;
+
   // the counts
   bool drop = false;
+  LetGo own;
   for (uint32_t i = tid; i < total; i += PT) {
     const int b = owner(first, B, i), at = (int)(i - first[b]);
     const bool full = at < length[b] >> a.shift;
@@ -387,12 +427,14 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
     drop |= children[b] == 0;
     if (change == 0) continue;
     const int page = a.table[(int64_t)b * a.max_pages + at];
-    if ((uint32_t)page < (uint32_t)a.n_pages) atomicAdd(a.refs + page, change);
+    if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+    const int was = atomicAdd(a.refs + page, change);
+    if (i == (uint32_t)tid && children[b] == 0) own = {page, b, was};
   }
   int n_free = n_free0;
   if (__syncthreads_or(drop))
     n_free += push_unheld(a.table, a.refs, a.free, B, a.max_pages, a.n_pages, n_free, first, total,
-                          [&](int b) { return children[b] == 0; }, part);
+                          [&](int b) { return children[b] == 0; }, own, part);
 
   // a page for each further child of a partly filled last page
   uint32_t asked[2] = {0, 0};
@@ -412,7 +454,7 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
       }
       continue;
     }
-    const int src = a.table[(int64_t)p * a.max_pages + (length[p] >> a.shift)], dst = a.free[n_free - 1 - at];
+    const int src = b0 ? last_page(b) : own_last, dst = a.free[n_free - 1 - at];
     fresh[b] = dst;
     const bool known = (uint32_t)src < (uint32_t)a.n_pages && (uint32_t)dst < (uint32_t)a.n_pages;
     if ((uint32_t)dst < (uint32_t)a.n_pages) set_count(a.refs, dst, 1);
@@ -426,29 +468,16 @@ __global__ __launch_bounds__(PT) void k_cache_reorder(CacheReorderArgs a) {
     a.moves[0] = copies;
     a.n_free[0] = n_free - copies;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
-  if ((tid & 63) == 0) part[0][tid >> 6] = (uint32_t)longest;
-  __syncthreads();
-  for (int w = 0; w < PT / 64; ++w) longest = max(longest, (int)part[0][w]);
-
-  // the tables
-  const int cols = max(1, min(longest, PT * RE / B)), n = B * cols;
   for (int c0 = 0; c0 < longest; c0 += cols) {
-    int value[RE];
+    if (c0 > 0) read(c0);
+    settled_barrier();  // everything is read before any of it changes
 #pragma unroll
     for (int u = 0; u < RE; ++u) {
-      const int e = tid + u * PT, b = e / cols, col = c0 + e % cols;
-      const int p = e < n ? parent[b] : -1;
-      value[u] = INT_MIN;
+      const int e = tid + u * PT;
+      if (e >= n) continue;
+      const int b = e / cols, col = c0 + e % cols, p = parent[b];
       if (p < 0 || (p == b && fresh[b] < 0) || col >= pages_of(length[p], a.shift)) continue;
-      value[u] = fresh[b] >= 0 && col == length[p] >> a.shift ? fresh[b] : a.table[(int64_t)p * a.max_pages + col];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < RE; ++u) {
-      const int e = tid + u * PT, b = e / cols, col = c0 + e % cols;
-      if (e < n && value[u] != INT_MIN) a.table[(int64_t)b * a.max_pages + col] = value[u];
+      a.table[(int64_t)b * a.max_pages + col] = fresh[b] >= 0 && col == length[p] >> a.shift ? fresh[b] : value[u];
     }
   }
   for (int b = tid; b < B; b += PT) a.len[b] = parent[b] >= 0 ? length[parent[b]] : 0;
