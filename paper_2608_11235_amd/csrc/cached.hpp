@@ -41,7 +41,7 @@ struct BeamPlan {
   int parts, chunk;
   size_t bytes;
 };
-constexpr int64_t BEAM_MAX_ROWS = 1 << 22;  // a workgroup of 512 threads a row and range
+constexpr int64_t BEAM_MAX_ROWS = 1 << 22;  // a launch's workgroups
 constexpr int BEAM_MAX = CORA_BEAM_MAX;  // beams of a request, and candidates kept of it
 BeamPlan beam_plan(int B, int K, int V, int W, int num_cus);
 hipError_t launch_vocab_beam(BeamArgs a, const BeamPlan& p, void* ws, hipStream_t s);

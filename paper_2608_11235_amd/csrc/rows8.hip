@@ -139,7 +139,7 @@ __global__ __launch_bounds__(512) void k_quantize_rows(QuantizeArgs a) {
 }
 
 hipError_t launch_quantize_rows(const QuantizeArgs& a, R8Source from, hipStream_t s) {
-  const dim3 grid((unsigned)(r8_groups(a.rows) * r8_quads(a.cols)));  // below 2^23
+  const dim3 grid((unsigned)(r8_groups(a.rows) * r8_quads(a.cols)));  // below 2^23: 2^32 threads
   switch (from) {
     case R8_BF16: hipLaunchKernelGGL(k_quantize_rows<R8_BF16>, grid, dim3(512), 0, s, a); break;
     case R8_F32: hipLaunchKernelGGL(k_quantize_rows<R8_F32>, grid, dim3(512), 0, s, a); break;

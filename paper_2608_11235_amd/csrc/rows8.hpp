@@ -18,6 +18,7 @@ __host__ __device__ inline int r8_blocks(int cols) { return (cols + 127) / 128; 
 __host__ __device__ inline int r8_quads(int cols) { return (cols + 511) / 512; }
 constexpr int R8_MAX_COLS = 1 << 20, R8_MAX_ROWS = 1 << 27;
 constexpr int R8_MAX_PRODUCT_ROWS = 1 << 21, R8_MAX_PRODUCT_COLS = 1 << 25;  // a launch's workgroups
+constexpr int64_t R8_MAX_PRODUCT = 1LL << 40;  // tiles are counted in 31 bits, the smallest is 64 x 64
 
 // Where the quantized rows come from: bf16 or fp32 rows of stride ld; a layer's weights in 64 x 32 blocks; K panels
 // [cols / 32][rows][32] (cols % 32 == 0 in both); or silu(gate) * up of bf16 rows that hold 16 gate and 16 up

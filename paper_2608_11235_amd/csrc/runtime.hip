@@ -1351,8 +1351,8 @@ extern "C" cora_status cora_quantize_rows(const void* d_x, int32_t x_f32, int64_
   if (out->rows == 0) return CORA_OK;
   if (!d_x || ld < out->cols || (reinterpret_cast<uintptr_t>(d_x) & (x_f32 ? 3 : 1)) != 0)
     return fail(CORA_ERR_INVALID_ARG, "x must be given, aligned to its elements, ld >= cols");
-  if ((int64_t)out->rows * r8_quads(out->cols) >= 1 << 27)
-    return fail(CORA_ERR_UNSUPPORTED, "rows * ceil(cols / 512) must stay below 2^27");
+  if (r8_groups(out->rows) * r8_quads(out->cols) > most_workgroups(512))
+    return fail(CORA_ERR_UNSUPPORTED, "ceil(rows / 16) * ceil(cols / 512) must stay below 2^23");
   HIP_TRY(launch_quantize_rows(QuantizeArgs{d_x, ld, out->rows, out->cols, out->data, out->scale}, x_f32 ? R8_F32 : R8_BF16,
                                S(hip_stream)));
   return CORA_OK;
@@ -1365,6 +1365,7 @@ static cora_status check_product_sizes(int32_t M, int32_t N, int32_t cols) {
   if (cora_status e = check_rows8_sizes(N, cols)) return e;
   if (M > R8_MAX_PRODUCT_ROWS || N > R8_MAX_PRODUCT_COLS)
     return fail(CORA_ERR_UNSUPPORTED, "a product's M must not exceed 2^21, its N 2^25");
+  if ((int64_t)M * N > R8_MAX_PRODUCT) return fail(CORA_ERR_UNSUPPORTED, "a product's M * N must not exceed 2^40");
   return CORA_OK;
 }
 

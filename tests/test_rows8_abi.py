@@ -37,6 +37,7 @@ def test_quantize(lib):  # noqa: F811
     assert quantize(lib, x=FAKE + 1) == INVALID and quantize(lib, x=FAKE + 2, f32=1) == INVALID
     assert quantize(lib, rows8(lib, rows=1 << 27)) == UNSUPPORTED
     assert quantize(lib, rows8(lib, rows=1 << 20, cols=1 << 20), ld=1 << 20) == UNSUPPORTED
+    assert quantize(lib, rows8(lib, rows=(1 << 27) - 15, cols=1), ld=1) == UNSUPPORTED  # 2^23 workgroups of 512 threads
     assert quantize(lib, rows8(lib, rows=0, data=None, scale=None), x=None) == 0
     assert lib.load().cora_quantize_rows(FAKE, 0, 256, None, None) == INVALID
 
@@ -48,6 +49,7 @@ def test_product(lib):  # noqa: F811
     assert product(lib, w=rows8(lib, cols=128)) == INVALID
     assert product(lib, a=rows8(lib, rows=(1 << 21) + 1)) == UNSUPPORTED
     assert product(lib, w=rows8(lib, rows=(1 << 25) + 1)) == UNSUPPORTED
+    assert product(lib, a=rows8(lib, rows=1 << 20), w=rows8(lib, rows=(1 << 20) + 1), ld=1 << 21) == UNSUPPORTED
     assert product(lib, a=rows8(lib, rows=0, data=None, scale=None), out=None) == 0
     assert lib.load().cora_rows_product(None, None, None, FAKE, 0, 4, None, 0, None) == INVALID
 
