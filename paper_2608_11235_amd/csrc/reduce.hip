@@ -3,6 +3,7 @@
 // into what the next kernel reads.
 #include "common.hpp"
 #include "internal.hpp"
+#include "rows8.hpp"
 
 namespace cora {
 
@@ -12,12 +13,16 @@ namespace cora {
 // and the chunk count C (float4 chunks per thread, C * NT * 4 >= d) are compile-time, so
 // every partial and residual load of a thread is issued before the first add; rows of
 // 4096 take 1024 threads with one chunk each, which keeps the most loads in flight.
-template <int SPLITS, int C, int NT>
+// Q8: the bf16 rows leave in 8 bits; a chunk's 32 neighbouring threads hold a block's 128 columns, those
+// past the row zeros, up to the next multiple of 512 for the scales.  Rows up to the next multiple of 16 stay
+// unwritten: they reach no other row's results.
+template <int SPLITS, int C, int NT, bool Q8>
 __global__ __launch_bounds__(NT) void k_residual_norm(float* __restrict__ h,
                                                       const float* __restrict__ part,
                                                       int64_t slab, int d,
                                                       const float* __restrict__ w,
-                                                      uint16_t* __restrict__ out, float eps) {
+                                                      uint16_t* __restrict__ out, uint8_t* __restrict__ scale,
+                                                      float eps) {
   const int64_t r = blockIdx.x;
   float* x = h + r * d;
   const float* p = part + r * d;
@@ -65,7 +70,30 @@ __global__ __launch_bounds__(NT) void k_residual_norm(float* __restrict__ h,
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     const int c = (threadIdx.x + i * NT) * 4;
-    if (c < d) {
+    if constexpr (Q8) {
+      float y[4] = {0.f, 0.f, 0.f, 0.f};
+      if (c < d) {
+        const float4 g = *reinterpret_cast<const float4*>(w + c);
+        const float z[4] = {v[i].x * inv * g.x, v[i].y * inv * g.y, v[i].z * inv * g.z, v[i].w * inv * g.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = bf16_bits_to_f32((uint16_t)f32_to_bf16_bits(z[e]));
+      }
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t b = __float_as_uint(y[e]) & 0x7fffffffu;
+        if (b >= 0x7f800000u) y[e] = __uint_as_float(0x7fc00000u);
+        else most = max(most, b);
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+      const int byte = r8_scale_byte(most), block = c >> 7, nk = r8_blocks(d), nq = r8_quads(d);
+      const float by = r8_inverse(byte);
+      if (block < nk)
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(out) + ((r >> 4) * nk + block) * R8_BLOCK + (c >> 6 & 1) * 1024 +
+                                     (c >> 4 & 3) * 256 + (r & 15) * 16 + (c & 15)) = r8_pack(y[0] * by, y[1] * by, y[2] * by, y[3] * by);
+      if ((c & 127) == 0 && block < 4 * nq) scale[((r >> 4) * nq + (block >> 2)) * 64 + (r & 15) * 4 + (block & 3)] = (uint8_t)byte;
+    } else if (c < d) {
       const float4 g = *reinterpret_cast<const float4*>(w + c);
       u32x2_t q;
       q.x = pack_bf16x2(v[i].x * inv * g.x, v[i].y * inv * g.y);
@@ -75,10 +103,10 @@ __global__ __launch_bounds__(NT) void k_residual_norm(float* __restrict__ h,
   }
 }
 
-template <int SPLITS>
+template <int SPLITS, bool Q8>
 static void residual_norm_c(int d4, dim3 grid, hipStream_t s, float* h, const float* part,
-                            int64_t slab, int d, const float* w, uint16_t* out, float eps) {
-#define RN(C_, NT_) hipLaunchKernelGGL((k_residual_norm<SPLITS, C_, NT_>), grid, dim3(NT_), 0, s, h, part, slab, d, w, out, eps)
+                            int64_t slab, int d, const float* w, uint16_t* out, uint8_t* scale, float eps) {
+#define RN(C_, NT_) hipLaunchKernelGGL((k_residual_norm<SPLITS, C_, NT_, Q8>), grid, dim3(NT_), 0, s, h, part, slab, d, w, out, scale, eps)
   if (d4 <= 256) RN(1, 256);
   else if (d4 <= 512) RN(1, 512);
   else if (d4 <= 1024) RN(1, 1024);
@@ -86,8 +114,9 @@ static void residual_norm_c(int d4, dim3 grid, hipStream_t s, float* h, const fl
 #undef RN
 }
 
-hipError_t launch_residual_norm(float* h, const float* part, int splits, int rows, int d,
-                                const float* w, uint16_t* out, float eps, hipStream_t s) {
+template <bool Q8>
+static hipError_t residual_norm(float* h, const float* part, int splits, int rows, int d,
+                                const float* w, uint16_t* out, uint8_t* scale, float eps, hipStream_t s) {
   if (rows == 0) return hipSuccess;
   if (d % 32 != 0 || d > RESIDUAL_NORM_MAX_D) return hipErrorInvalidValue;
   static_assert(RESIDUAL_NORM_MAX_D <= 2 * 1024 * 4, "at most 2 float4 chunks per thread");
@@ -95,13 +124,23 @@ hipError_t launch_residual_norm(float* h, const float* part, int splits, int row
   const int64_t slab = (int64_t)rows * d;
   const dim3 grid(rows);
   switch (splits) {
-    case 1: residual_norm_c<1>(d4, grid, s, h, part, slab, d, w, out, eps); break;
-    case 2: residual_norm_c<2>(d4, grid, s, h, part, slab, d, w, out, eps); break;
-    case 4: residual_norm_c<4>(d4, grid, s, h, part, slab, d, w, out, eps); break;
-    case 8: residual_norm_c<8>(d4, grid, s, h, part, slab, d, w, out, eps); break;
+    case 1: residual_norm_c<1, Q8>(d4, grid, s, h, part, slab, d, w, out, scale, eps); break;
+    case 2: residual_norm_c<2, Q8>(d4, grid, s, h, part, slab, d, w, out, scale, eps); break;
+    case 4: residual_norm_c<4, Q8>(d4, grid, s, h, part, slab, d, w, out, scale, eps); break;
+    case 8: residual_norm_c<8, Q8>(d4, grid, s, h, part, slab, d, w, out, scale, eps); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
+}
+
+hipError_t launch_residual_norm(float* h, const float* part, int splits, int rows, int d,
+                                const float* w, uint16_t* out, float eps, hipStream_t s) {
+  return residual_norm<false>(h, part, splits, rows, d, w, out, nullptr, eps, s);
+}
+
+hipError_t launch_residual_norm_rows8(float* h, const float* part, int splits, int rows, int d, const float* w,
+                                      uint8_t* data, uint8_t* scale, float eps, hipStream_t s) {
+  return residual_norm<true>(h, part, splits, rows, d, w, reinterpret_cast<uint16_t*>(data), scale, eps, s);
 }
 
 // QKV projection partials -> q and k with rotate-half RoPE, v transposed.  q/k columns are

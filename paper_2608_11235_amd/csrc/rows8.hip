@@ -86,22 +86,12 @@ __device__ __forceinline__ void load_chunk(const QuantizeArgs& a, int64_t row, i
   }
 }
 
-// The scale's byte of a block whose largest finite magnitude has these bits: with most = m 2^p, 1 <= m < 2,
-// the exponent is p - 8 for m <= 1.75 (448 = 1.75 2^8), else p - 7; no less than -127.
-__device__ __forceinline__ int scale_byte(uint32_t most) {
-  const int e = (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return most == 0 ? 127 : max(e, 0);
-}
-
 // 16 values to e4m3: what is not finite becomes NaN
 __device__ __forceinline__ u32x4_t pack_e4m3(const float (&x)[16], float by) {
   u32x4_t q;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * t] * by, x[4 * t + 1] * by, w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * t + 2] * by, x[4 * t + 3] * by, w, true);
-    q[t] = (uint32_t)w;
+    q[t] = r8_pack(x[4 * t] * by, x[4 * t + 1] * by, x[4 * t + 2] * by, x[4 * t + 3] * by);
   }
   return q;
 }
@@ -130,9 +120,9 @@ __global__ __launch_bounds__(512) void k_quantize_rows(QuantizeArgs a) {
   }
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
-  const int e = scale_byte(most);  // 127 + exponent
+  const int e = r8_scale_byte(most);  // 127 + exponent
   if (kb < nk) {
-    const u32x4_t q = pack_e4m3(x, __uint_as_float((uint32_t)(254 - e) << 23));
+    const u32x4_t q = pack_e4m3(x, r8_inverse(e));
     *reinterpret_cast<u32x4_t*>(a.data + (group * nk + kb) * R8_BLOCK + c * 256 + r * 16) = q;
   }
   if (c == 0) a.scale[(group * nq + quad) * 64 + r * 4 + (tid >> 7)] = (uint8_t)e;
@@ -764,20 +754,30 @@ static hipError_t run_tiles(const Rows8ProductArgs& a, const Rows8Plan& p, hipSt
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_rows8_product(const Rows8ProductArgs& in, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s) {
+static hipError_t run(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, bool wide, hipStream_t s) {
+  if (p.few && a.M > rows8_few_rows(wide)) return hipErrorInvalidValue;
+  if (p.few) return wide ? run_few<OUT_F32, true>(a, p, s) : (f32 ? run_few<OUT_F32, false>(a, p, s) : run_few<OUT_BF16, false>(a, p, s));
+  return wide ? run_tiles<OUT_F32, true>(a, p, s) : (f32 ? run_tiles<OUT_F32, false>(a, p, s) : run_tiles<OUT_BF16, false>(a, p, s));
+}
+
+static Rows8ProductArgs into_parts(const Rows8ProductArgs& in, float* ws) {
   Rows8ProductArgs a = in;
-  if (p.splits > 1) {  // into the workspace first
-    a.out = ws;
-    a.ld = (in.N + 3) / 4 * 4;
-    a.bias = nullptr;
-  }
-  const bool out_f32 = f32 || p.splits > 1;
-  if (p.few && in.M > rows8_few_rows(wide)) return hipErrorInvalidValue;
-  hipError_t e;
-  if (p.few) e = wide ? run_few<OUT_F32, true>(a, p, s) : (out_f32 ? run_few<OUT_F32, false>(a, p, s) : run_few<OUT_BF16, false>(a, p, s));
-  else e = wide ? run_tiles<OUT_F32, true>(a, p, s) : (out_f32 ? run_tiles<OUT_F32, false>(a, p, s) : run_tiles<OUT_BF16, false>(a, p, s));
-  if (e == hipSuccess && p.splits > 1) e = fold(in, ws, p.splits, (int)a.ld, f32, s);
-  return e;
+  a.out = ws;
+  a.ld = (in.N + 3) / 4 * 4;
+  a.bias = nullptr;
+  return a;
+}
+
+hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s) {
+  if (p.splits == 1) return run(a, p, f32, wide, s);
+  const Rows8ProductArgs parts = into_parts(a, ws);
+  if (hipError_t e = run(parts, p, true, wide, s)) return e;
+  return fold(a, ws, p.splits, (int)parts.ld, f32, s);
+}
+
+hipError_t launch_rows8_parts(const Rows8ProductArgs& a, const Rows8Plan& p, float* ws, hipStream_t s) {
+  if (p.splits < 2 || a.N % 4 != 0) return hipErrorInvalidValue;
+  return run(into_parts(a, ws), p, true, false, s);
 }
 
 }  // namespace cora

@@ -20,6 +20,20 @@ constexpr int R8_MAX_COLS = 1 << 20, R8_MAX_ROWS = 1 << 27;
 constexpr int R8_MAX_PRODUCT_ROWS = 1 << 21, R8_MAX_PRODUCT_COLS = 1 << 25;  // a launch's workgroups
 constexpr int64_t R8_MAX_PRODUCT = 1LL << 40;  // tiles are counted in 31 bits, the smallest is 64 x 64
 
+// The scale's byte of a block whose largest finite magnitude has these bits: with most = m 2^p, 1 <= m < 2,
+// the exponent is p - 8 for m <= 1.75 (448 = 1.75 2^8), else p - 7; no less than -127.
+__device__ __forceinline__ int r8_scale_byte(uint32_t most) {
+  const int e = (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return most == 0 ? 127 : max(e, 0);
+}
+// one over that scale
+__device__ __forceinline__ float r8_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+__device__ __forceinline__ uint32_t r8_pack(float x0, float x1, float x2, float x3) {
+  int w = 0;
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, w, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, w, true);
+}
+
 // Where the quantized rows come from: bf16 or fp32 rows of stride ld; a layer's weights in 64 x 32 blocks; K panels
 // [cols / 32][rows][32] (cols % 32 == 0 in both); or silu(gate) * up of bf16 rows that hold 16 gate and 16 up
 // columns in turn.
@@ -55,5 +69,11 @@ Rows8Plan rows8_plan_few(int M, int N, int K, int nb, int sq, int ranges, bool w
 int rows8_few_rows(bool wide);  // of a launch
 Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus);
 hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s);
+// the same without bias, the splits' fp32 sums [splits][M][N] left in the workspace (splits > 1, N % 4 == 0)
+hipError_t launch_rows8_parts(const Rows8ProductArgs& a, const Rows8Plan& p, float* ws, hipStream_t s);
+
+// launch_residual_norm (internal.hpp) with its bf16 rows in 8 bits
+hipError_t launch_residual_norm_rows8(float* h, const float* part, int splits, int rows, int d, const float* w,
+                                      uint8_t* data, uint8_t* scale, float eps, hipStream_t s);
 
 }  // namespace cora

@@ -1216,13 +1216,13 @@ static cora_status begin_cached_pass(cora_model* m, const CachedPass& x, const i
   return CORA_OK;
 }
 
-// Layer l from the projection's `splits` fp32 partials in the split-K workspace to the attention's output in m->attn.
-static cora_status cached_attention(cora_model* m, const CachedPass& x, size_t l, int splits, hipStream_t s) {
+// Layer l from the projection's fp32 partials [splits][rows][qkv_n] to the attention's output in m->attn.
+static cora_status cached_attention(cora_model* m, const CachedPass& x, size_t l, const float* sums, int splits, hipStream_t s) {
   const auto& c = m->cfg;
   const int M = x.ch->rows, hd = c.head_dim;
   const size_t layer_elems = cache_layer_elems(x.cache);
   CacheStoreArgs st{};
-  st.xf = m->splitk_ws; st.ld = m->qkv_n; st.slab = (int64_t)M * m->qkv_n; st.splits = splits;
+  st.xf = sums; st.ld = m->qkv_n; st.slab = (int64_t)M * m->qkv_n; st.splits = splits;
   st.bias = m->layers[l].bqkv;
   st.rows = M; st.H = c.n_heads; st.Hkv = c.n_kv_heads; st.shift = page_shift(x.cache->page_size);
   st.n_slots = x.cache->n_pages * x.cache->page_size;
@@ -1270,7 +1270,7 @@ extern "C" cora_status cora_forward_cached(cora_model* m, const cora_cache* cach
   for (size_t l = 0; l < m->layers.size(); ++l) {
     GemmArgs g{m->a, m->layers[l].wqkv, W_BLOCKS, M, m->qkv_n, d, m->splitk_ws, m->qkv_n, nullptr, 1.0f};
     HIP_TRY(launch_gemm(EPI_PART_F32, g, gp, s));
-    if (cora_status e = cached_attention(m, x, l, gp.splits, s)) return e;
+    if (cora_status e = cached_attention(m, x, l, m->splitk_ws, gp.splits, s)) return e;
     if (cora_status e = after_attention(m, l, M, M, s)) return e;
   }
   const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
@@ -1508,25 +1508,47 @@ extern "C" cora_status cora_forward_quantized(cora_model* m, const void* d_weigh
   const CachedPass x = cached_pass(m, cache, p, ch, max_count, max_len, causal);
   Matrix8 dims[4];
   layer_matrices(m, dims);
-  // out = the 8-bit rows of `from` times matrix j of layer l, in fp32 (sums of the 8-bit instruction) or bf16
-  auto product = [&](size_t l, int j, const void* from, int64_t ld, R8Source how, void* out, bool f32) -> cora_status {
+  const auto quantize = [&](const void* from, int64_t ld, int cols, R8Source how) {
+    return launch_quantize_rows(QuantizeArgs{from, ld, M, cols, ws + q.data, ws + q.scale}, how, s);
+  };
+  // The 8-bit rows times matrix j of layer l (sums of the 8-bit instruction): into `bf16`, or as fp32 for the next kernel,
+  // which adds the sums of split columns itself where it knows their number.
+  const float* sums = nullptr;
+  int splits = 1;
+  auto product = [&](size_t l, int j, uint16_t* bf16) -> cora_status {
     const Matrix8& w = dims[j];
     const uint8_t* at = matrix8(m, const_cast<void*>(d_weights), l, j);
-    HIP_TRY(launch_quantize_rows(QuantizeArgs{from, ld, M, w.cols, ws + q.data, ws + q.scale}, how, s));
-    const Rows8ProductArgs g{ws + q.data, ws + q.scale, at, at + align_up(r8_data_bytes(w.rows, w.cols)), M, w.rows, w.cols, nullptr, out, w.rows};
-    HIP_TRY(launch_rows8_product(g, rows8_plan(M, w.rows, w.cols, false, m->num_cus), f32, false, reinterpret_cast<float*>(ws + q.parts), s));
+    const Rows8Plan pl = rows8_plan(M, w.rows, w.cols, false, m->num_cus);
+    float* parts = reinterpret_cast<float*>(ws + q.parts);
+    Rows8ProductArgs g{ws + q.data, ws + q.scale, at, at + align_up(r8_data_bytes(w.rows, w.cols)), M, w.rows, w.cols, nullptr, bf16, w.rows};
+    if (!bf16 && (pl.splits == 2 || pl.splits == 4 || pl.splits == 8)) {
+      sums = parts;
+      splits = pl.splits;
+      HIP_TRY(launch_rows8_parts(g, pl, parts, s));
+      return CORA_OK;
+    }
+    if (!bf16) g.out = m->splitk_ws;
+    sums = m->splitk_ws;
+    splits = 1;
+    HIP_TRY(launch_rows8_product(g, pl, !bf16, false, parts, s));
     return CORA_OK;
   };
   if (cora_status e = begin_cached_pass(m, x, d_tokens, s)) return e;
   for (size_t l = 0; l < m->layers.size(); ++l) {
-    if (cora_status e = product(l, 0, m->a, 0, R8_PANELS, m->splitk_ws, true)) return e;
-    if (cora_status e = cached_attention(m, x, l, 1, s)) return e;
-    if (cora_status e = product(l, 1, m->attn, 0, R8_PANELS, m->splitk_ws, true)) return e;
-    HIP_TRY(launch_residual_norm(m->h, m->splitk_ws, 1, M, d, m->ones, m->a, m->cfg.rms_eps, s));
-    if (cora_status e = product(l, 2, m->a, 0, R8_PANELS, gate_up, false)) return e;
-    if (cora_status e = product(l, 3, gate_up, 2 * m->f_pad, R8_SWIGLU, m->splitk_ws, true)) return e;
+    if (l == 0) HIP_TRY(quantize(m->a, 0, d, R8_PANELS));
+    if (cora_status e = product(l, 0, nullptr)) return e;
+    if (cora_status e = cached_attention(m, x, l, sums, splits, s)) return e;
+    HIP_TRY(quantize(m->attn, 0, m->hq, R8_PANELS));
+    if (cora_status e = product(l, 1, nullptr)) return e;
+    HIP_TRY(launch_residual_norm_rows8(m->h, sums, splits, M, d, m->ones, ws + q.data, ws + q.scale, m->cfg.rms_eps, s));
+    if (cora_status e = product(l, 2, gate_up)) return e;
+    HIP_TRY(quantize(gate_up, 2 * m->f_pad, m->f_pad, R8_SWIGLU));
+    if (cora_status e = product(l, 3, nullptr)) return e;
     // the last layer's output is normalised by the LM head
-    HIP_TRY(launch_residual_norm(m->h, m->splitk_ws, 1, M, d, m->ones, l + 1 < m->layers.size() ? m->a : nullptr, m->cfg.rms_eps, s));
+    if (l + 1 < m->layers.size())
+      HIP_TRY(launch_residual_norm_rows8(m->h, sums, splits, M, d, m->ones, ws + q.data, ws + q.scale, m->cfg.rms_eps, s));
+    else
+      HIP_TRY(launch_residual_norm(m->h, sums, splits, M, d, m->ones, nullptr, m->cfg.rms_eps, s));
   }
   const RowSel all{0, 0, 0, 0, 0, 0, 0, nullptr};
   return lm_head(m, all, M, M, d_logits, s);
