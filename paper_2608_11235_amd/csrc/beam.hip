@@ -78,7 +78,7 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 
 }  // namespace
 
-// 1024 x 152064 in 70 us (4.4 TB/s) with four workgroups of 256 threads a CU: without the candidates 59, without the exponentials 63,
+// 1024 x 152064 in 69 us (4.5 TB/s) with four workgroups of 256 threads a CU: without the candidates 59, without the exponentials 63,
 // without both 57.  Slower were two workgroups of 512 (80), 32 logits a thread (105, in scratch memory), lists of the wavefronts' own
 // in place of the workgroup's barriers (94: four times the candidates) and a cut at 64 or 128 held candidates (72, 79).
 // Of a row's logits those in whole 16-byte blocks are loaded eight at a time, a tile ahead; the up to seven on either
@@ -92,13 +92,21 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x / a.parts;
   const int part = blockIdx.x % a.parts;
-  const float score = a.score[row];
-  if (!(score > -INFINITY) || (a.done && a.done[row])) return;  // no candidates, or the one without logits
+  const bool none = !(a.score[row] > -INFINITY) || (a.done && a.done[row]);  // no candidates, or the one without logits
   const int W = a.W, trim = max(32, 2 * W);  // held candidates beyond which they are cut down to the W best
   const uint16_t* x = a.logits + row * a.ld;
   const int head = min(a.V, (int)(-((uintptr_t)x >> 1) & 7)), blocks = (a.V - head) / 8;
-  const int b0 = min(part * a.chunk, blocks), b1 = min(b0 + a.chunk, blocks);  // blocks of this range
+  const int tiles = (blocks + TILE / 8 - 1) / (TILE / 8);
+  const int b0 = tiles * part / a.parts * (TILE / 8), b1 = min(tiles * (part + 1) / a.parts * (TILE / 8), blocks);  // blocks of this range
   const u32x4_t* body = reinterpret_cast<const u32x4_t*>(x + head);
+  u32x4_t next[BE / 8] = {};
+  auto load = [&](int at, bool any) {
+    if (!any) return;
+#pragma unroll
+    for (int h = 0; h < BE / 8; ++h) next[h] = body[min(at + h * BT + tid, b1 - 1)];
+  };
+  load(b0, b0 < b1);  // on its way while the score is looked at
+  if (none) return;
   if (tid == 0) {
     least = 0x80ull << 32;  // LOWEST
     held = 0;
@@ -124,13 +132,6 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   if (side == a.mask_id) side = -1;
   const float sv = side >= 0 ? bf16_bits_to_f32(x[side]) : -INFINITY;
 
-  u32x4_t next[BE / 8] = {};
-  auto load = [&](int at, bool any) {
-    if (!any) return;
-#pragma unroll
-    for (int h = 0; h < BE / 8; ++h) next[h] = body[min(at + h * BT + tid, b1 - 1)];
-  };
-  load(b0, b0 < b1);
   uint64_t bound = 0x80ull << 32;
   float bound_v = LOWEST;
   for (int base = b0; base == b0 || base < b1; base += BT * BE / 8) {
@@ -244,28 +245,29 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
     }
     __syncthreads();
   }
-  const int n = keep_best(list, held, W, &least);
-  uint64_t* out = a.best + (row * a.parts + part) * W;
-  for (int i = tid; i < W; i += BT) out[i] = i < n ? list[i] : 0;
-
-  // the range's sum, relative to the largest thread's reference
-  double at = k == 1.f ? (double)ref : -(double)o * 0.6931471805599453, top = at;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d, 64));
-  if (lane == 0) tops[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < BT / 64; ++w) top = fmax(top, tops[w]);
-  double sum = (double)s * (k == 1.f ? 1.0 : 1.0 - LOG2E_OFF * ref) * exp(at - top);
+  // a wavefront's sum, relative to the largest of its threads' references
+  double top = warp_max(ref), sum = (double)s * (k == 1.f ? 1.0 : 1.0 - LOG2E_OFF * ref) * exp((k == 1.f ? (double)ref : -(double)o * 0.6931471805599453) - top);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-  if (lane == 0) sums[wave] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    sum = 0;
-    for (int w = 0; w < BT / 64; ++w) sum += sums[w];
-    a.stats[2 * (row * a.parts + part)] = top;
-    a.stats[2 * (row * a.parts + part) + 1] = sum;
+  if (lane == 0) {
+    tops[wave] = top;
+    sums[wave] = sum;
+  }
+  const int n = keep_best(list, held, W, &least);  // its barriers come before what follows
+  uint64_t* out = a.best + (row * a.parts + part) * W;
+  for (int i = tid; i < W; i += BT) out[i] = i < n ? list[i] : 0;
+  if (wave == BT / 64 - 1) {
+    const double t = tops[lane & (BT / 64 - 1)];
+    top = t;
+#pragma unroll
+    for (int d = BT / 128; d > 0; d >>= 1) top = fmax(top, __shfl_xor(top, d, 64));
+    sum = sums[lane & (BT / 64 - 1)] * exp(t - top);
+#pragma unroll
+    for (int d = BT / 128; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if (lane == 0) {
+      a.stats[2 * (row * a.parts + part)] = top;
+      a.stats[2 * (row * a.parts + part) + 1] = sum;
+    }
   }
 }
 
@@ -394,21 +396,18 @@ __global__ __launch_bounds__(512) void k_beam_merge(BeamArgs a) {
   }
 }
 
-// Ranges of a row: enough workgroups for the chip, ranges of a tile at the least; in blocks of eight ids.
+// Ranges of a row: enough workgroups for the chip, of whole tiles.
 BeamPlan beam_plan(int B, int K, int V, int W, int num_cus) {
   const int64_t rows = (int64_t)B * K;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>(4 * num_cus / std::max<int64_t>(rows, 1), (V + TILE - 1) / TILE));
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(4 * num_cus / std::max<int64_t>(rows, 1), (V + TILE - 1) / TILE));
   BeamPlan p;
-  const int blocks = std::max(1, V / 8);
-  p.chunk = (int)((blocks + parts - 1) / parts);
-  p.parts = (blocks + p.chunk - 1) / p.chunk;
+  p.parts = (int)parts;
   p.bytes = (size_t)rows * p.parts * (16 + 8 * (size_t)W);
   return p;
 }
 
 hipError_t launch_vocab_beam(BeamArgs a, const BeamPlan& p, void* ws, hipStream_t s) {
   a.parts = p.parts;
-  a.chunk = p.chunk;
   a.stats = static_cast<double*>(ws);
   a.best = reinterpret_cast<uint64_t*>(a.stats + 2 * (size_t)a.B * a.K * a.parts);
   hipLaunchKernelGGL(k_beam_rows, dim3((unsigned)((int64_t)a.B * a.K * a.parts)), dim3(BT), 0, s, a);

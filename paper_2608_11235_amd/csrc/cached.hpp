@@ -33,12 +33,12 @@ struct BeamArgs {
   const float* score; const uint8_t* done;
   int done_token, W;
   int32_t *token, *parent; float* next;  // [B][W]
-  int parts, chunk;                      // set by the launcher: a row in `parts` ranges of `chunk` ids
+  int parts;                             // set by the launcher: ranges of a row
   double* stats;                         // of each range: a power of two and the sum of exp relative to it
   uint64_t* best;                        // and its W largest logits
 };
 struct BeamPlan {
-  int parts, chunk;
+  int parts;
   size_t bytes;
 };
 constexpr int64_t BEAM_MAX_ROWS = 1 << 22;  // a launch's workgroups
