@@ -25,6 +25,10 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 // 16 bytes at any alignment of two
 struct __attribute__((packed, aligned(2))) bf16x8_any { uint16_t v[8]; };
 struct __attribute__((packed, aligned(4))) f32x4_any { float v[4]; };
+// 8, 12 and 16 bytes at any alignment of four, which is all that stores of more than a dword need
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4_out __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ void unpack16(const uint16_t* p, float (&x)[16]) {  // aligned to 16 bytes
 #pragma unroll
@@ -194,8 +198,8 @@ constexpr int OOB = 0x7fffffff;  // an offset past every buffer: zeros, no traff
 constexpr int STREAM = 2;        // cache policy of weights that are read once a call: nontemporal
 enum { OUT_BF16 = 0, OUT_F32 = 1 };
 
-// bias, rounding and store of columns col .. col + 3 of a row
-template <int OUT>
+// bias, rounding and store of columns col .. col + 3 of a row; ANY: wide stores at any alignment of the elements
+template <int OUT, bool ANY = true>
 __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, int col, f32x4_t x) {
   if (g.bias) {
 #pragma unroll
@@ -204,8 +208,8 @@ __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, i
   }
   if constexpr (OUT == OUT_F32) {
     float* dst = static_cast<float*>(g.out) + row * g.ld + col;
-    if (col + 3 < g.N && (g.ld & 3) == 0 && ((uintptr_t)g.out & 15) == 0) {
-      *reinterpret_cast<f32x4_t*>(dst) = x;
+    if (col + 3 < g.N && (ANY || ((g.ld & 3) == 0 && ((uintptr_t)g.out & 15) == 0))) {
+      *reinterpret_cast<f32x4_out*>(dst) = x;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -213,8 +217,12 @@ __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, i
     }
   } else {
     uint16_t* dst = static_cast<uint16_t*>(g.out) + row * g.ld + col;
-    if (col + 3 < g.N && (g.ld & 3) == 0 && ((uintptr_t)g.out & 7) == 0) {
-      *reinterpret_cast<u32x2_t*>(dst) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    if (col + 3 < g.N && (ANY ? ((uintptr_t)dst & 3) == 0 : (g.ld & 3) == 0 && ((uintptr_t)g.out & 7) == 0)) {
+      *reinterpret_cast<u32x2_any*>(dst) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    } else if (ANY && col + 3 < g.N) {
+      dst[0] = (uint16_t)f32_to_bf16_bits(x[0]);
+      *reinterpret_cast<uint32_t*>(dst + 1) = pack_bf16x2(x[1], x[2]);
+      dst[3] = (uint16_t)f32_to_bf16_bits(x[3]);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -336,6 +344,11 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
   }
 }
 
+// bf16 rows that start at dwords, and tiles that can write others by 16 bytes a lane too: the largest ones have no
+// registers left for it (with the code for it 4096 x 37888 x 3584 took 1130 us, 468 without)
+__host__ __device__ __forceinline__ bool starts_at_dwords(const Rows8ProductArgs& g) { return (g.ld & 1) == 0 && ((uintptr_t)g.out & 3) == 0; }
+constexpr bool r8_any_rows(int TM, int TN) { return TM * TN < 32; }
+
 // Tiles of many rows.  A workgroup of WM x WN wavefronts goes through tiles of BM x BN; a wavefront owns TM x TN
 // blocks of 16 x 16.
 //
@@ -440,7 +453,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   constexpr int RUNS = 16 * CB * 2 / 64, STORES = OUT == OUT_BF16 ? TM * (TN / CB) * RUNS : 0;
   int st = 0;           // stage of the section at hand
   int this_by = 0;      // WIDE: byte of its scales
-  bool late = false;    // a tile's stores, all STORES of them, were issued since the loads that a barrier waits for
+  bool late = false;    // a tile's stores, STORES of them or more, were issued since the loads that a barrier waits for
+  constexpr bool ANY_ROWS = r8_any_rows(TM, TN);
   // FIRST: of a tile; by: byte of the next section's scales
   auto section = [&](auto first_c, int by) {
     constexpr bool FIRST = decltype(first_c)::value;
@@ -530,7 +544,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
     tile_of(item % tiles, num_m, tiles, tm, tn);
     const int64_t row0 = (int64_t)scalar(tm) * BM + wm * TM * 16, slab = (int64_t)scalar(item / tiles) * g.M;
     const int col0 = scalar(tn) * BN + wn * TN * 16;
-    late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N && (g.ld & 7) == 0 && ((uintptr_t)g.out & 15) == 0;
+    late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N && (ANY_ROWS || starts_at_dwords(g));
     if (late) {
       constexpr int PITCH = CB * 32 + 16;
       char* scr = stages + ST * STAGE + wave * 16 * PITCH;
@@ -558,8 +572,26 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
 #pragma unroll
           for (int u = 0; u < RUNS; ++u) {
             constexpr int RPR = 16 / RUNS;  // rows of a run of 64 lanes
-            *reinterpret_cast<u32x4_t*>(dst + (int64_t)(i * 16 + u * RPR) * g.ld + j0 * 16) =
-                *reinterpret_cast<const u32x4_t*>(scr + (u * RPR + lane / (CB * 2)) * PITCH + lane % (CB * 2) * 16);
+            const char* from = scr + (u * RPR + lane / (CB * 2)) * PITCH + lane % (CB * 2) * 16;
+            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from);
+            uint16_t* to = dst + (int64_t)(i * 16 + u * RPR) * g.ld + j0 * 16;
+            if constexpr (!ANY_ROWS) {
+              *reinterpret_cast<u32x4_any*>(to) = x;
+            } else if (starts_at_dwords(g)) {
+              *reinterpret_cast<u32x4_any*>(to) = x;
+            } else {
+              // a row that starts between two dwords: from its second element on, the next lane's first one with it
+              const uint32_t more = *reinterpret_cast<const uint32_t*>(from + 16);  // the last lane: its row's padding
+              const bool odd = (uintptr_t)to & 2, last = lane % (CB * 2) == CB * 2 - 1;
+              const u32x4_t y = {x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16 | more << 16};
+              if (!(odd && last)) *reinterpret_cast<u32x4_any*>(to + (odd ? 1 : 0)) = odd ? y : x;
+              if (odd && lane % (CB * 2) == 0) to[0] = (uint16_t)x[0];
+              if (odd && last) {
+                *reinterpret_cast<u32x2_any*>(to + 1) = u32x2_t{y[0], y[1]};
+                *reinterpret_cast<uint32_t*>(to + 5) = y[2];
+                to[7] = (uint16_t)(x[3] >> 16);
+              }
+            }
           }
           wave_lds_sync();
         }
@@ -571,7 +603,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
         for (int j = 0; j < TN; ++j) {
           const int64_t r = row0 + i * 16 + r16;
           const int c = col0 + j * 16 + 4 * g4;
-          if (r < g.M && c < g.N) store4<OUT>(g, slab + r, c, acc[i][j]);
+          if (r < g.M && c < g.N) store4<OUT, ANY_ROWS>(g, slab + r, c, acc[i][j]);
         }
     }
   }
@@ -668,6 +700,7 @@ Rows8Plan rows8_plan_few(int M, int N, int K, int nb, int sq, int ranges, bool w
 Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus) {
   Rows8Plan p{};
   p.cfg = cfg;
+  p.num_cus = num_cus;
   p.splits = splits;
   p.ws_floats = splits > 1 ? (size_t)splits * M * ((N + 3) / 4 * 4) : 0;
   const R8Shape sh = r8_shape(cfg);
@@ -677,6 +710,8 @@ Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus
 }
 
 // Splits of a product by tiles leave no more than this in the workspace.
+// Two launches have to promise this much: what the estimate gives them is 4 % more than they keep.
+constexpr double R8_REST_US = 1.5, R8_REST_GAIN = 0.92;
 constexpr int64_t R8_MOST_PARTS = 1 << 26;
 
 Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
@@ -705,7 +740,30 @@ Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
       if (best_us < 0 || us < best_us) { best_cfg = c; best_splits = splits; best_us = us; }
     }
   }
-  return rows8_plan_tiles(M, N, K, best_cfg, best_splits, num_cus);
+  // The last round of tiles may leave most CUs idle: whole rounds of one config, then the other weight rows as a product
+  // of their own (4096 x 37888 x 3584, 9.25 rounds: FIGURE).
+  int n_first = N, rest_cfg = 0;
+  double rest_us = 0;
+  for (int c = 0; c < R8_CONFIGS; ++c) {
+    if (wide && c != 3 && c != 5) continue;
+    const R8Shape sh = r8_shape(c);
+    const int64_t num_m = (M + sh.bm - 1) / sh.bm, slots = (int64_t)num_cus * sh.per_cu, items = num_m * ((N + sh.bn - 1) / sh.bn);
+    const int64_t first = items / slots * slots / num_m * sh.bn;
+    if (first < 1 || first >= N) continue;
+    const double us = tiles_us(M, (int)first, K, c, 1, wide, num_cus);
+    for (int d = 0; d < R8_CONFIGS; ++d) {
+      if (wide && d != 3 && d != 5) continue;
+      const double both = us + R8_REST_US + tiles_us(M, N - (int)first, K, d, 1, wide, num_cus);
+      if (both < R8_REST_GAIN * best_us && (n_first == N || both < rest_us)) { best_cfg = c; best_splits = 1; n_first = (int)first; rest_cfg = d; rest_us = both; }
+    }
+  }
+  Rows8Plan p = rows8_plan_tiles(M, n_first, K, best_cfg, best_splits, num_cus);
+  if (n_first < N) {
+    p.rest = N - n_first;
+    p.rest_cfg = rest_cfg;
+    p.rest_grid = rows8_plan_tiles(M, p.rest, K, rest_cfg, 1, num_cus).grid;
+  }
+  return p;
 }
 
 static hipError_t fold(const Rows8ProductArgs& a, const float* parts, int splits, int ld, bool f32, hipStream_t s) {
@@ -737,7 +795,9 @@ static hipError_t run_few(const Rows8ProductArgs& a, const Rows8Plan& p, hipStre
   X(5, 2, 2, 2, 2, 4, 2, 2)
 
 template <int OUT, bool WIDE>
-static hipError_t run_tiles(const Rows8ProductArgs& a, const Rows8Plan& p, hipStream_t s) {
+static hipError_t run_tiles(const Rows8ProductArgs& a, Rows8Plan p, hipStream_t s) {
+  if (OUT == OUT_BF16 && p.cfg == 0 && !starts_at_dwords(a))  // tiles that can: 3579 x 24991 x 2241 FIG us, 301 without
+    p = rows8_plan_tiles(a.M, a.N, a.K, 1, 1, p.num_cus);
 #define X(C, WM, WN, TM, TN, ST, CB, PER, ...)                                                                           \
   if (p.cfg == C) {                                                                                                      \
     constexpr unsigned LDS = ST * (WM * TM + WN * TN) * 16 * 132 + WM * WN * 16 * (CB * 32 + 16);                        \
@@ -769,6 +829,23 @@ static Rows8ProductArgs into_parts(const Rows8ProductArgs& in, float* ws) {
 }
 
 hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, bool f32, bool wide, float* ws, hipStream_t s) {
+  if (p.rest) {
+    Rows8ProductArgs g = a;
+    g.N = a.N - p.rest;
+    if (hipError_t e = run(g, p, f32, wide, s)) return e;
+    const int nk = r8_blocks(a.K), nq = r8_quads(a.K);
+    g.w += (int64_t)(g.N / 16) * nk * R8_BLOCK;  // g.N: whole tiles
+    g.w_scale += (int64_t)(g.N / 16) * nq * 64;
+    if (g.bias) g.bias += g.N;
+    g.out = static_cast<char*>(g.out) + (int64_t)g.N * (f32 ? 4 : 2);
+    g.N = p.rest;
+    Rows8Plan rest{};
+    rest.cfg = p.rest_cfg;
+    rest.grid = p.rest_grid;
+    rest.num_cus = p.num_cus;
+    rest.splits = 1;
+    return run(g, rest, f32, wide, s);
+  }
   if (p.splits == 1) return run(a, p, f32, wide, s);
   const Rows8ProductArgs parts = into_parts(a, ws);
   if (hipError_t e = run(parts, p, true, wide, s)) return e;
