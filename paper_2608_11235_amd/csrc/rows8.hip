@@ -25,9 +25,9 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 // 16 bytes at any alignment of two
 struct __attribute__((packed, aligned(2))) bf16x8_any { uint16_t v[8]; };
 struct __attribute__((packed, aligned(4))) f32x4_any { float v[4]; };
-// 8, 12 and 16 bytes at any alignment of four, which is all that stores of more than a dword need
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4)));
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+// Stores at any alignment of the elements, one instruction each (3579 x 24990 x 2241 180 us, element by element 302).
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_out __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ void unpack16(const uint16_t* p, float (&x)[16]) {  // aligned to 16 bytes
@@ -198,8 +198,8 @@ constexpr int OOB = 0x7fffffff;  // an offset past every buffer: zeros, no traff
 constexpr int STREAM = 2;        // cache policy of weights that are read once a call: nontemporal
 enum { OUT_BF16 = 0, OUT_F32 = 1 };
 
-// bias, rounding and store of columns col .. col + 3 of a row; ANY: wide stores at any alignment of the elements
-template <int OUT, bool ANY = true>
+// bias, rounding and store of columns col .. col + 3 of a row
+template <int OUT>
 __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, int col, f32x4_t x) {
   if (g.bias) {
 #pragma unroll
@@ -208,7 +208,7 @@ __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, i
   }
   if constexpr (OUT == OUT_F32) {
     float* dst = static_cast<float*>(g.out) + row * g.ld + col;
-    if (col + 3 < g.N && (ANY || ((g.ld & 3) == 0 && ((uintptr_t)g.out & 15) == 0))) {
+    if (col + 3 < g.N) {
       *reinterpret_cast<f32x4_out*>(dst) = x;
     } else {
 #pragma unroll
@@ -217,12 +217,8 @@ __device__ __forceinline__ void store4(const Rows8ProductArgs& g, int64_t row, i
     }
   } else {
     uint16_t* dst = static_cast<uint16_t*>(g.out) + row * g.ld + col;
-    if (col + 3 < g.N && (ANY ? ((uintptr_t)dst & 3) == 0 : (g.ld & 3) == 0 && ((uintptr_t)g.out & 7) == 0)) {
+    if (col + 3 < g.N) {
       *reinterpret_cast<u32x2_any*>(dst) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-    } else if (ANY && col + 3 < g.N) {
-      dst[0] = (uint16_t)f32_to_bf16_bits(x[0]);
-      *reinterpret_cast<uint32_t*>(dst + 1) = pack_bf16x2(x[1], x[2]);
-      dst[3] = (uint16_t)f32_to_bf16_bits(x[3]);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -344,11 +340,6 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
   }
 }
 
-// bf16 rows that start at dwords, and tiles that can write others by 16 bytes a lane too: the largest ones have no
-// registers left for it (with the code for it 4096 x 37888 x 3584 took 1130 us, 468 without)
-__host__ __device__ __forceinline__ bool starts_at_dwords(const Rows8ProductArgs& g) { return (g.ld & 1) == 0 && ((uintptr_t)g.out & 3) == 0; }
-constexpr bool r8_any_rows(int TM, int TN) { return TM * TN < 32; }
-
 // Tiles of many rows.  A workgroup of WM x WN wavefronts goes through tiles of BM x BN; a wavefront owns TM x TN
 // blocks of 16 x 16.
 //
@@ -454,7 +445,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   int st = 0;           // stage of the section at hand
   int this_by = 0;      // WIDE: byte of its scales
   bool late = false;    // a tile's stores, STORES of them or more, were issued since the loads that a barrier waits for
-  constexpr bool ANY_ROWS = r8_any_rows(TM, TN);
   // FIRST: of a tile; by: byte of the next section's scales
   auto section = [&](auto first_c, int by) {
     constexpr bool FIRST = decltype(first_c)::value;
@@ -544,7 +534,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
     tile_of(item % tiles, num_m, tiles, tm, tn);
     const int64_t row0 = (int64_t)scalar(tm) * BM + wm * TM * 16, slab = (int64_t)scalar(item / tiles) * g.M;
     const int col0 = scalar(tn) * BN + wn * TN * 16;
-    late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N && (ANY_ROWS || starts_at_dwords(g));
+    late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N;
     if (late) {
       constexpr int PITCH = CB * 32 + 16;
       char* scr = stages + ST * STAGE + wave * 16 * PITCH;
@@ -572,26 +562,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
 #pragma unroll
           for (int u = 0; u < RUNS; ++u) {
             constexpr int RPR = 16 / RUNS;  // rows of a run of 64 lanes
-            const char* from = scr + (u * RPR + lane / (CB * 2)) * PITCH + lane % (CB * 2) * 16;
-            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from);
-            uint16_t* to = dst + (int64_t)(i * 16 + u * RPR) * g.ld + j0 * 16;
-            if constexpr (!ANY_ROWS) {
-              *reinterpret_cast<u32x4_any*>(to) = x;
-            } else if (starts_at_dwords(g)) {
-              *reinterpret_cast<u32x4_any*>(to) = x;
-            } else {
-              // a row that starts between two dwords: from its second element on, the next lane's first one with it
-              const uint32_t more = *reinterpret_cast<const uint32_t*>(from + 16);  // the last lane: its row's padding
-              const bool odd = (uintptr_t)to & 2, last = lane % (CB * 2) == CB * 2 - 1;
-              const u32x4_t y = {x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16 | more << 16};
-              if (!(odd && last)) *reinterpret_cast<u32x4_any*>(to + (odd ? 1 : 0)) = odd ? y : x;
-              if (odd && lane % (CB * 2) == 0) to[0] = (uint16_t)x[0];
-              if (odd && last) {
-                *reinterpret_cast<u32x2_any*>(to + 1) = u32x2_t{y[0], y[1]};
-                *reinterpret_cast<uint32_t*>(to + 5) = y[2];
-                to[7] = (uint16_t)(x[3] >> 16);
-              }
-            }
+            *reinterpret_cast<u32x4_any*>(dst + (int64_t)(i * 16 + u * RPR) * g.ld + j0 * 16) =
+                *reinterpret_cast<const u32x4_t*>(scr + (u * RPR + lane / (CB * 2)) * PITCH + lane % (CB * 2) * 16);
           }
           wave_lds_sync();
         }
@@ -603,7 +575,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
         for (int j = 0; j < TN; ++j) {
           const int64_t r = row0 + i * 16 + r16;
           const int c = col0 + j * 16 + 4 * g4;
-          if (r < g.M && c < g.N) store4<OUT, ANY_ROWS>(g, slab + r, c, acc[i][j]);
+          if (r < g.M && c < g.N) store4<OUT>(g, slab + r, c, acc[i][j]);
         }
     }
   }
@@ -700,7 +672,6 @@ Rows8Plan rows8_plan_few(int M, int N, int K, int nb, int sq, int ranges, bool w
 Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus) {
   Rows8Plan p{};
   p.cfg = cfg;
-  p.num_cus = num_cus;
   p.splits = splits;
   p.ws_floats = splits > 1 ? (size_t)splits * M * ((N + 3) / 4 * 4) : 0;
   const R8Shape sh = r8_shape(cfg);
@@ -741,7 +712,7 @@ Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
     }
   }
   // The last round of tiles may leave most CUs idle: whole rounds of one config, then the other weight rows as a product
-  // of their own (4096 x 37888 x 3584, 9.25 rounds: FIGURE).
+  // of their own (3804 x 4493 x 11519, 1.05 rounds of 256 x 256 tiles: 162 us, as 256 x 128 tiles alone 240).
   int n_first = N, rest_cfg = 0;
   double rest_us = 0;
   for (int c = 0; c < R8_CONFIGS; ++c) {
@@ -795,9 +766,7 @@ static hipError_t run_few(const Rows8ProductArgs& a, const Rows8Plan& p, hipStre
   X(5, 2, 2, 2, 2, 4, 2, 2)
 
 template <int OUT, bool WIDE>
-static hipError_t run_tiles(const Rows8ProductArgs& a, Rows8Plan p, hipStream_t s) {
-  if (OUT == OUT_BF16 && p.cfg == 0 && !starts_at_dwords(a))  // tiles that can: 3579 x 24991 x 2241 FIG us, 301 without
-    p = rows8_plan_tiles(a.M, a.N, a.K, 1, 1, p.num_cus);
+static hipError_t run_tiles(const Rows8ProductArgs& a, const Rows8Plan& p, hipStream_t s) {
 #define X(C, WM, WN, TM, TN, ST, CB, PER, ...)                                                                           \
   if (p.cfg == C) {                                                                                                      \
     constexpr unsigned LDS = ST * (WM * TM + WN * TN) * 16 * 132 + WM * WN * 16 * (CB * 32 + 16);                        \
@@ -842,7 +811,6 @@ hipError_t launch_rows8_product(const Rows8ProductArgs& a, const Rows8Plan& p, b
     Rows8Plan rest{};
     rest.cfg = p.rest_cfg;
     rest.grid = p.rest_grid;
-    rest.num_cus = p.num_cus;
     rest.splits = 1;
     return run(g, rest, f32, wide, s);
   }

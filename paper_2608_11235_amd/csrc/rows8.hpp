@@ -62,7 +62,6 @@ struct Rows8Plan {
   int splits;            // workgroups along the columns, whose sums a second kernel adds
   size_t ws_floats;
   int rest, rest_cfg, rest_grid;  // tiles: the last weight rows that go to a launch of other tiles, or 0
-  int num_cus;                    // what it was made for
 };
 struct Rows8Few { int kw; };
 // wide: results in fp32 with sums of 32 bits (else those of the 8-bit instruction)

@@ -115,7 +115,7 @@ def rows(seed, R, K, spread=0.5):
 SHAPES = [(1, 1, 1), (1, 16, 128), (1, 5, 64), (2, 17, 129), (15, 100, 512), (16, 688, 256), (17, 257, 513),
           (31, 1, 1000), (32, 500, 4096), (33, 48, 640), (48, 63, 2048), (64, 1000, 1536), (65, 130, 127),
           (130, 65, 1024), (333, 1531, 1000), (257, 1, 300), (128, 128, 8192), (700, 520, 640), (4, 9000, 64),
-          (1024, 512, 1024), (2047, 300, 4097)]
+          (1024, 512, 1024), (2047, 300, 4097), (2533, 6750, 895), (2533, 6751, 895), (2346, 3703, 603)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
