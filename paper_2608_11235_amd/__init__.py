@@ -17,6 +17,7 @@ supplies device memory and the HIP stream only.
     cache_reorder(cache, parent)            the cache's requests go on as their parents, pages shared
     Rows8, quantize_rows, rows8_product     matrices in 8 bits, a power of two as the scale of each 128
                                             columns of a row, and their products
+    Model.quantize()                        the layers' matrices in 8 bits, for forward_cached(weights=...)
 """
 from .api import (  # noqa: F401
     Model, DecodeState, Sched, Gate, vocab_gate, vocab_gate_noalloc, model_cfg_from,
