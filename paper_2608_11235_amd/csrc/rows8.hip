@@ -729,6 +729,7 @@ Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
     const int64_t first = items / slots * slots / num_m * sh.bn;
     if (first < 1 || first >= N) continue;
     const double us = tiles_us(M, (int)first, K, c, 1, wide, num_cus);
+    if (us + R8_REST_US >= R8_REST_GAIN * best_us) continue;
     for (int d = 0; d < R8_CONFIGS; ++d) {
       if (wide && d != 3 && d != 5) continue;
       const double both = us + R8_REST_US + tiles_us(M, N - (int)first, K, d, 1, wide, num_cus);
