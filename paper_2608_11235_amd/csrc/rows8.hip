@@ -165,17 +165,17 @@ __device__ __forceinline__ f32x4_t mfma(i32x8_t w, i32x8_t a, f32x4_t acc, uint3
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, acc, 0, 0, U, (int)ws, U, (int)as);
 }
 
-// eight e4m3 numbers as bf16, which holds them exactly
-__device__ __forceinline__ bf16x8_t widened(uint32_t lo, uint32_t hi) {
-  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// eight e4m3 numbers times a power of two as bf16, which holds them exactly
+__device__ __forceinline__ bf16x8_t widened(uint32_t lo, uint32_t hi, float by) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true);
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // The same by the bf16 instruction, whose sums keep 32 bits: sum first, then the scales.  ws: the scales
 // of the lane's four weight rows.
 struct Wide { bf16x8_t k[4]; };
-__device__ __forceinline__ Wide widened(i32x8_t x) {
-  return Wide{{widened(x[0], x[1]), widened(x[2], x[3]), widened(x[4], x[5]), widened(x[6], x[7])}};
+__device__ __forceinline__ Wide widened(i32x8_t x, float by = 1.0f) {
+  return Wide{{widened(x[0], x[1], by), widened(x[2], x[3], by), widened(x[4], x[5], by), widened(x[6], x[7], by)}};
 }
 __device__ __forceinline__ f32x4_t mfma_wide(const Wide& w, const Wide& a, f32x4_t acc, u32x4_t ws, uint32_t as, int byte) {
   f32x4_t p = {0.f, 0.f, 0.f, 0.f};
@@ -358,8 +358,10 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
 // next tile's first loads (4096 x 37888 bf16 written alone in runs of 32 bytes 81 us, of 64 58 us, of 256 56 us).
 // Bound by the matrix cores and the power that they draw: 8192^3 bf16 in 400 us (2.75 PFLOP/s; on zeros 357),
 // 4096 x 37888 x 3584 in 475 (2.34: the cores busy for 66 % of the cycles), 2048 x 24576 x 4096 in 148 (2.8).
-// WIDE (sums of 32 bits): a section's fragments are widened to bf16 first, the activations all, a group of weight
-// rows at a time; they are free at once, and the barrier stands between.
+// WIDE (sums of 32 bits): a section's fragments are widened to bf16 first, times their scales, the activations all, a group
+// of weight rows at a time; they are free at once, and the barrier stands between.  Bound by the conversions beside the
+// matrix cores: 2048 x 12288 x 4096 in 182 us (1.13 PFLOP/s; 227 with the scales applied to each block's sums).  A tile with
+// a scale outside 2^-50 .. 2^50, whose products may leave the normal numbers, is made again that way, from memory.
 template <int WM, int WN, int TM, int TN, int ST, int CB, int OUT, bool WIDE>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArgs g, int splits) {
   constexpr int NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, GA = BM / 16, GB = BN / 16;
@@ -429,10 +431,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   // ---- the products
   f32x4_t acc[TM][TN];
   i32x8_t fa[TM], fb[TN];
-  std::conditional_t<WIDE, u32x4_t, uint32_t> sb[TN];  // WIDE: the dwords of the lane's four weight rows
+  uint32_t sb[TN];  // scales: the section's byte; WIDE: the dword
   uint32_t sa[TM];
   const int a_at = wm * TM * R8_BLOCK + lane * 16, b_at = (GA + wn * TN) * R8_BLOCK + lane * 16;
-  const int as_at = ROWS * 128 + (wm * TM * 16 + r16) * 4, bs_at = ROWS * 128 + (BM + wn * TN * 16 + (WIDE ? 4 * g4 : r16)) * 4;
+  const int as_at = ROWS * 128 + (wm * TM * 16 + r16) * 4, bs_at = ROWS * 128 + (BM + wn * TN * 16 + r16) * 4;
   auto frag = [&](int at) {
     return both(*reinterpret_cast<const u32x4_t*>(stages + at), *reinterpret_cast<const u32x4_t*>(stages + at + 1024));
   };
@@ -443,25 +445,29 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
   };
   auto read_b = [&](int st, int by, int j) {
     fb[j] = frag(st + b_at + j * R8_BLOCK);
-    if constexpr (WIDE) sb[j] = *reinterpret_cast<const u32x4_t*>(stages + st + bs_at + j * 64);
+    if constexpr (WIDE) sb[j] = *reinterpret_cast<const uint32_t*>(stages + st + bs_at + j * 64);
     else sb[j] = *reinterpret_cast<const uint8_t*>(stages + st + bs_at + by + j * 64);
   };
   constexpr int NM = TM * TN, HALF = TM / 2, BAR = NM / 2 >= 2 ? NM / 2 - 2 : 0;
   constexpr int RUNS = 16 * CB * 2 / 64, STORES = OUT == OUT_BF16 ? TM * (TN / CB) * RUNS : 0;
   int st = 0;           // stage of the section at hand
   int this_by = 0;      // WIDE: byte of its scales
+  uint32_t far = 0;     // WIDE: a scale of the tile's lies outside 2^-50 .. 2^50
   bool late = false;    // a tile's stores, STORES of them or more, were issued since the loads that a barrier waits for
   // FIRST: of a tile; by: byte of the next section's scales
   auto section = [&](auto first_c, int by) {
     constexpr bool FIRST = decltype(first_c)::value;
     const int nx = st + STAGE == ST * STAGE ? 0 : st + STAGE;
     if constexpr (WIDE) {
+      auto scale_of = [&](uint32_t dword) {
+        const uint32_t e = dword >> 8 * this_by & 255;
+        far |= e - 77 > 100 ? 1 : 0;
+        return __uint_as_float(e << 23);
+      };
       Wide a[TM];
-      uint32_t as[TM];
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        a[i] = widened(fa[i]);
-        as[i] = sa[i];
+        a[i] = widened(fa[i], scale_of(sa[i]));
         if constexpr (FIRST) {
 #pragma unroll
           for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -474,15 +480,16 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
       for (int i = 0; i < TM; ++i) read_a(nx, by, i);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const Wide w = widened(fb[j]);
-        const u32x4_t ws = sb[j];
+        const Wide w = widened(fb[j], scale_of(sb[j]));
         read_b(nx, by, j);
 #pragma unroll
         for (int t = 0; t < ALL; ++t)
           if (t * TN / ALL == j) issue((uint32_t)st, t);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) acc[i][j] = mfma_wide(w, a[i], acc[i][j], ws, as[i], this_by);
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.k[t], a[i].k[t], acc[i][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
       this_by = by;
@@ -540,6 +547,31 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
     tile_of(item % tiles, num_m, tiles, tm, tn);
     const int64_t row0 = (int64_t)scalar(tm) * BM + wm * TM * 16, slab = (int64_t)scalar(item / tiles) * g.M;
     const int col0 = scalar(tn) * BN + wn * TN * 16;
+    if constexpr (WIDE) {
+      if (__ballot(far != 0)) {  // products of such scales' numbers may leave the normal ones: the tile again, its blocks' sums first, then the scales
+        const int64_t ga = (int64_t)scalar(tm) * GA + wm * TM, gb = (int64_t)scalar(tn) * GB + wn * TN;
+        const int64_t a_end = (g.M + 15) / 16 - 1, b_end = (g.N + 15) / 16 - 1;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const int64_t ra = min(ga + i, a_end), rb = min(gb + j, b_end);  // past the last group: it again
+            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+            for (int k = k0; k < k1; ++k) {
+              const uint8_t *pa = g.a + (ra * nk_all + k) * R8_BLOCK + lane * 16, *pw = g.w + (rb * nk_all + k) * R8_BLOCK + lane * 16;
+              const i32x8_t a = both(*reinterpret_cast<const u32x4_t*>(pa), *reinterpret_cast<const u32x4_t*>(pa + 1024));
+              const i32x8_t w = both(*reinterpret_cast<const u32x4_t*>(pw), *reinterpret_cast<const u32x4_t*>(pw + 1024));
+              const uint8_t *qa = g.a_scale + (ra * nq + (k >> 2)) * 64, *qw = g.w_scale + (rb * nq + (k >> 2)) * 64;
+              u32x4_t ws;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) ws[e] = qw[(4 * g4 + e) * 4 + (k & 3)];
+              x = mfma_wide(widened(w), widened(a), x, ws, qa[r16 * 4 + (k & 3)], 0);
+            }
+            acc[i][j] = x;
+          }
+      }
+      far = 0;
+    }
     late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N;
     if (late) {
       constexpr int PITCH = CB * 32 + 16;
@@ -631,12 +663,13 @@ static R8Shape r8_shape(int cfg) {
 // latency a section and the chip's throughput, plus what a tile takes besides; the stream of weights, a fifth of which
 // goes beside it; the sums of split columns.  Fitted to all configs and splits of 209 shapes (80 to 4096 rows, 688 to
 // 37888 weight rows, 1000 to 12288 columns; 12 % off in the mean).  What it picks is on average 1 %, at most 15 % slower
-// than the fastest of these.  Sections of 32-bit sums take 2.15 times as long.
+// than the fastest of these.  Sections of 32-bit sums count 1.95 times (their measured 1.7 picks
+// plans that are 1 % slower).
 static double tiles_us(int M, int N, int K, int cfg, int splits, bool wide, int num_cus) {
   R8Shape sh = r8_shape(cfg);
   if (wide) {
-    sh.section_us *= 2.15;
-    sh.cu_us *= 2.15;
+    sh.section_us *= 1.95;
+    sh.cu_us *= 1.95;
   }
   const double sections = (double)r8_blocks(K) / splits;
   const int64_t items = (int64_t)((M + sh.bm - 1) / sh.bm) * ((N + sh.bn - 1) / sh.bn) * splits, slots = (int64_t)num_cus * sh.per_cu;
