@@ -156,6 +156,21 @@ def test_scales_far_apart(M, up, down):
         check_product(quantize_rows(x), quantize_rows(y), dtype=dtype)
 
 
+@pytest.mark.parametrize("M,N,K", [(20, 40, 900), (300, 257, 513), (333, 500, 4096), (1000, 900, 700)])
+@pytest.mark.parametrize("up,down", [(0, 0), (90, 0), (-90, 0), (90, -110), (-90, -50), (50, 51), (-51, 60)])
+def test_far_scales_in_a_few_rows(M, N, K, up, down):
+    """Rows of numbers far from one, some of whose products fall below the normal numbers, beside ordinary ones."""
+    require_gpu()
+    log_case(f"far rows 2^{up}, 2^{down}: {M} x {N} x {K}")
+    x, y = torch.randn((M, K), generator=gen(6), device="cuda"), torch.randn((N, K), generator=gen(7), device="cuda")
+    x[M // 2] *= 2.0 ** up
+    x[M // 3, :K // 2] *= 2.0 ** up
+    y[N // 2] *= 2.0 ** down
+    y[N - 1, K // 3:] *= 2.0 ** down
+    for dtype in (torch.bfloat16, torch.float32):
+        check_product(quantize_rows(x), quantize_rows(y), dtype=dtype)
+
+
 @pytest.mark.parametrize("M,N,K", [(7, 33, 300), (70, 130, 1000), (300, 257, 513)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("pad,offset", [(0, 0), (1, 1), (4, 4), (3, 2)])
