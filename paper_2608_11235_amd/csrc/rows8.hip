@@ -7,7 +7,7 @@
 //
 // Products: v_mfma_scale_f32_16x16x128_f8f6f4 takes the 128 columns of a block with both scales and adds in
 // fp32.  It adds a block's products with the bits below 2^-13 of the largest one left out (1.6e-5 of the
-// result in the mean where all are of a size, 5e-5 where they are not: a fortieth of bf16's half step), so results
+// result in the mean where all are of a size, 5e-5 where they are not: an eightieth of bf16's half step), so results
 // that leave in fp32 to the caller are made by the bf16 instruction, which keeps 32 bits (4e-8), at half
 // its rate.  The weights are its first operand, so that a lane holds one row of the result and four columns.
 #include <algorithm>
