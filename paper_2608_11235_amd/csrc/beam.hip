@@ -23,6 +23,7 @@ constexpr int BE = 16;          // logits of a thread and tile
 constexpr int TILE = BT * BE;
 constexpr int CAP = 512;       // held candidates of a range
 constexpr int RANK = 8;          // compared at a time
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 constexpr float LOWEST = -3.3895313892515355e38f;  // bf16's lowest finite number
 // LOG2E's own error, relative: a sum of 2^(v LOG2E) is that of exp(v (1 + this)), which for the terms that count,
 // those near the largest, is a factor 1 + this times v
@@ -81,8 +82,8 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 // 1024 x 152064 in 69 us (4.5 TB/s) with four workgroups of 256 threads a CU: without the candidates 59, without the exponentials 63,
 // without both 57.  Slower were two workgroups of 512 (80), 32 logits a thread (105, in scratch memory), lists of the wavefronts' own
 // in place of the workgroup's barriers (94: four times the candidates) and a cut at 64 or 128 held candidates (72, 79).
-// Of a row's logits those in whole 16-byte blocks are loaded eight at a time, a tile ahead; the up to seven on either
-// side are one each of the first threads', before the first tile.
+// A row's logits are loaded eight at a time, a tile ahead, whatever its alignment, so that equal rows have equal sums wherever
+// they lie; the up to seven behind are one each of the first threads', before the first tile.
 __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   __shared__ __attribute__((aligned(16))) uint64_t list[CAP + RANK];
   __shared__ uint64_t least;      // candidates below it are out
@@ -95,10 +96,10 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
   const bool none = !(a.score[row] > -INFINITY) || (a.done && a.done[row]);  // no candidates, or the one without logits
   const int W = a.W, trim = max(32, 2 * W);  // held candidates beyond which they are cut down to the W best
   const uint16_t* x = a.logits + row * a.ld;
-  const int head = min(a.V, (int)(-((uintptr_t)x >> 1) & 7)), blocks = (a.V - head) / 8;
+  const int blocks = a.V / 8;
   const int tiles = (blocks + TILE / 8 - 1) / (TILE / 8);
   const int b0 = tiles * part / a.parts * (TILE / 8), b1 = min(tiles * (part + 1) / a.parts * (TILE / 8), blocks);  // blocks of this range
-  const u32x4_t* body = reinterpret_cast<const u32x4_t*>(x + head);
+  const u32x4_any* body = reinterpret_cast<const u32x4_any*>(x);
   u32x4_t next[BE / 8] = {};
   auto load = [&](int at, bool any) {
     if (!any) return;
@@ -125,10 +126,8 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
     s = was_k == LOG2E && k == LOG2E ? s * fast_exp2(o - was_o) : s * fast_exp2((was - ref) * LOG2E);
   };
 
-  // the logit beside the blocks that this thread has, if any
-  int side = -1;
-  if (part == 0 && tid < head) side = tid;
-  if (part == a.parts - 1 && tid >= 8 && tid - 8 < a.V - head - 8 * blocks) side = head + 8 * blocks + tid - 8;
+  // the logit behind the blocks that this thread has, if any
+  int side = part == a.parts - 1 && tid < a.V - 8 * blocks ? 8 * blocks + tid : -1;
   if (side == a.mask_id) side = -1;
   const float sv = side >= 0 ? bf16_bits_to_f32(x[side]) : -INFINITY;
 
@@ -138,11 +137,11 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
     u32x4_t cur[BE / 8];
     float m8[BE / 8];
     const bool first = base == b0, any = b0 < b1;
-    const int id0 = head + 8 * (base + tid);  // of the first logit; those of cur[h] are BT * 8 h behind
+    const int id0 = 8 * (base + tid);  // of the first logit; those of cur[h] are BT * 8 h behind
 #pragma unroll
     for (int h = 0; h < BE / 8; ++h) cur[h] = next[h];
     load(min(base + BT * BE / 8, max(b1 - 1, 0)), any);  // past the last tile: not used
-    if (base + BT * BE / 8 > b1 || (uint32_t)(a.mask_id - head - 8 * base) < (uint32_t)TILE) {  // the last tile, or the mask's
+    if (base + BT * BE / 8 > b1 || (uint32_t)(a.mask_id - 8 * base) < (uint32_t)TILE) {  // the last tile, or the mask's
 #pragma unroll
       for (int h = 0; h < BE / 8; ++h) {
         int at = base + h * BT + tid >= b1 ? INT_MIN : a.mask_id - id0 - h * BT * 8;  // which of the eight is out; INT_MIN: all
@@ -198,7 +197,7 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
       bound = t > bound ? t : bound;
       bound_v = of_ordered((uint32_t)(bound >> 32));
       if (tid == 0) least = bound;
-      if (side >= 0 && candidate(ordered(sv), side) >= bound) list[atomicAdd(&held, 1)] = candidate(ordered(sv), side);  // 14 at the most
+      if (side >= 0 && candidate(ordered(sv), side) >= bound) list[atomicAdd(&held, 1)] = candidate(ordered(sv), side);  // 7 at the most
     }
     auto offer = [&]() {
 #pragma unroll
@@ -231,7 +230,7 @@ __global__ __launch_bounds__(BT, 4) void k_beam_rows(BeamArgs a) {
       cut(CAP);
       for (int i = tid; i < W; i += BT) {
         const int id = id_of(list[i]);
-        if (id >= head + 8 * base && id < head + 8 * b1) list[i] = 0;
+        if (id >= 8 * base && id < 8 * b1) list[i] = 0;
       }
       if (tid == 0) held = W;
       __syncthreads();
