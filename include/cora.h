@@ -293,8 +293,9 @@ cora_status cora_vocab_gate_sampled(const uint16_t *d_logits, int32_t n_rows, in
  * unchanged.  A beam whose score is -inf, +inf or NaN has none, nor has one without an allowed id or with a NaN or
  * +inf at one.  In the order of falling scores, equal ones by beam, then by falling logit, then by id,
  * the first W of a request go to d_token, d_parent (the row r) and d_next (the score) [B, W]; places
- * left over get token -1, parent -1 and -inf.  Sums and scores are 64-bit beyond a thread's own terms, so that the
- * order is that of the numbers to about 1e-7; equal rows have equal sums, wherever they lie.  mask_id = -1: no id is left out.  1 <= K, W <= CORA_BEAM_MAX,
+ * left over get token -1, parent -1 and -inf.  16 terms at a time are added in fp32, these sums and the scores in 64 bits:
+ * a row's log sum is off by 1e-7 or so (by arithmetic less than 7e-7 for V <= 2^18, 1.5e-6 for any V), the same for equal rows,
+ * and the order that of scores further apart than two of these.  mask_id = -1: no id is left out.  1 <= K, W <= CORA_BEAM_MAX,
  * V <= 2^30, B K <= 2^22.  The outputs overlap no input.
  * workspace of cora_vocab_beam_workspace bytes, 16-byte aligned: used from this call's start to its end on the
  * stream, contents not kept; calls that may overlap and captured graphs that may run at once need one
