@@ -196,6 +196,9 @@ __device__ __forceinline__ void each(std::integer_sequence<int, U...>, F&& f) {
   (f(std::integral_constant<int, U>{}), ...);
 }
 
+// a scale's byte outside 2^-50 .. 2^50
+__device__ __forceinline__ uint32_t is_far(uint32_t byte) { return byte - 77 > 100 ? 1 : 0; }
+
 constexpr int OOB = 0x7fffffff;  // an offset past every buffer: zeros, no traffic
 constexpr int STREAM = 2;        // cache policy of weights that are read once a call: nontemporal
 enum { OUT_BF16 = 0, OUT_F32 = 1 };
@@ -360,8 +363,8 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
 // 4096 x 37888 x 3584 in 475 (2.34: the cores busy for 66 % of the cycles), 2048 x 24576 x 4096 in 148 (2.8).
 // WIDE (sums of 32 bits): a section's fragments are widened to bf16 first, times their scales, the activations all, a group
 // of weight rows at a time; they are free at once, and the barrier stands between.  Bound by the conversions beside the
-// matrix cores: 2048 x 12288 x 4096 in 182 us (1.13 PFLOP/s; 227 with the scales applied to each block's sums).  A tile with
-// a scale outside 2^-50 .. 2^50, whose products may leave the normal numbers, is made again that way, from memory.
+// matrix cores: 2048 x 12288 x 4096 in 182 us (1.13 PFLOP/s; 227 with the scales applied to each block's sums).  The results of
+// rows with a scale outside 2^-50 .. 2^50, whose products may leave the normal numbers, are made again that way, from memory.
 template <int WM, int WN, int TM, int TN, int ST, int CB, int OUT, bool WIDE>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArgs g, int splits) {
   constexpr int NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, GA = BM / 16, GB = BN / 16;
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
     if constexpr (WIDE) {
       auto scale_of = [&](uint32_t dword) {
         const uint32_t e = dword >> 8 * this_by & 255;
-        far |= e - 77 > 100 ? 1 : 0;
+        far |= is_far(e);
         return __uint_as_float(e << 23);
       };
       Wide a[TM];
@@ -547,31 +550,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
     tile_of(item % tiles, num_m, tiles, tm, tn);
     const int64_t row0 = (int64_t)scalar(tm) * BM + wm * TM * 16, slab = (int64_t)scalar(item / tiles) * g.M;
     const int col0 = scalar(tn) * BN + wn * TN * 16;
-    if constexpr (WIDE) {
-      if (__ballot(far != 0)) {  // products of such scales' numbers may leave the normal ones: the tile again, its blocks' sums first, then the scales
-        const int64_t ga = (int64_t)scalar(tm) * GA + wm * TM, gb = (int64_t)scalar(tn) * GB + wn * TN;
-        const int64_t a_end = (g.M + 15) / 16 - 1, b_end = (g.N + 15) / 16 - 1;
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            const int64_t ra = min(ga + i, a_end), rb = min(gb + j, b_end);  // past the last group: it again
-            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-            for (int k = k0; k < k1; ++k) {
-              const uint8_t *pa = g.a + (ra * nk_all + k) * R8_BLOCK + lane * 16, *pw = g.w + (rb * nk_all + k) * R8_BLOCK + lane * 16;
-              const i32x8_t a = both(*reinterpret_cast<const u32x4_t*>(pa), *reinterpret_cast<const u32x4_t*>(pa + 1024));
-              const i32x8_t w = both(*reinterpret_cast<const u32x4_t*>(pw), *reinterpret_cast<const u32x4_t*>(pw + 1024));
-              const uint8_t *qa = g.a_scale + (ra * nq + (k >> 2)) * 64, *qw = g.w_scale + (rb * nq + (k >> 2)) * 64;
-              u32x4_t ws;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) ws[e] = qw[(4 * g4 + e) * 4 + (k & 3)];
-              x = mfma_wide(widened(w), widened(a), x, ws, qa[r16 * 4 + (k & 3)], 0);
-            }
-            acc[i][j] = x;
-          }
-      }
-      far = 0;
-    }
     late = OUT == OUT_BF16 && row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N;
     if (late) {
       constexpr int PITCH = CB * 32 + 16;
@@ -615,6 +593,41 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_rows8_tiles(Rows8ProductArg
           const int c = col0 + j * 16 + 4 * g4;
           if (r < g.M && c < g.N) store4<OUT>(g, slab + r, c, acc[i][j]);
         }
+    }
+    if constexpr (WIDE) {
+      // Products of such scales' numbers may leave the normal ones: the tile again, its blocks' sums first, then the scales, over the
+      // results of rows that have such a scale.  The others keep theirs, so that no row's bits depend on another's numbers.
+      if (__builtin_expect(__ballot(far != 0) != 0, 0)) {
+        const int64_t ga = row0 / 16, gb = col0 / 16, a_end = (g.M + 15) / 16 - 1, b_end = (g.N + 15) / 16 - 1;
+#pragma unroll 1
+        for (int t = 0; t < TM * TN; ++t) {
+          const int64_t ra = min(ga + t / TN, a_end), rb = min(gb + t % TN, b_end);  // past the last group: it again, not stored
+          f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+          uint32_t again = 0;  // bit e: column e's
+#pragma unroll 1
+          for (int k = k0; k < k1; ++k) {
+            const uint8_t *pa = g.a + (ra * nk_all + k) * R8_BLOCK + lane * 16, *pw = g.w + (rb * nk_all + k) * R8_BLOCK + lane * 16;
+            const i32x8_t a = both(*reinterpret_cast<const u32x4_t*>(pa), *reinterpret_cast<const u32x4_t*>(pa + 1024));
+            const i32x8_t w = both(*reinterpret_cast<const u32x4_t*>(pw), *reinterpret_cast<const u32x4_t*>(pw + 1024));
+            const uint8_t *qa = g.a_scale + (ra * nq + (k >> 2)) * 64, *qw = g.w_scale + (rb * nq + (k >> 2)) * 64;
+            const uint32_t as = qa[r16 * 4 + (k & 3)];
+            u32x4_t ws;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              ws[e] = qw[(4 * g4 + e) * 4 + (k & 3)];
+              again |= (is_far(ws[e]) | is_far(as)) << e;
+            }
+            x = mfma_wide(widened(w), widened(a), x, ws, as, 0);
+          }
+          const int64_t r = row0 + t / TN * 16 + r16;
+          const int c = col0 + t % TN * 16 + 4 * g4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (again >> e & 1 && r < g.M && c + e < g.N)
+              static_cast<float*>(g.out)[(slab + r) * g.ld + c + e] = x[e] + (g.bias ? g.bias[c + e] : 0.f);
+        }
+      }
+      far = 0;
     }
   }
   wait_vm<0>();
