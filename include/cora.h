@@ -436,7 +436,8 @@ cora_status cora_forward_cached(cora_model *model, const cora_cache *cache, cons
  *   data:  ((r/16) nb + c/128) 2048 + (c%128 / 64) 1024 + (c/16 % 4) 256 + (r%16) 16 + c%16
  * and its scale, the exponent + 127, at
  *   scale: ((r/16) nq + c/512) 64 + (r%16) 4 + c/128 % 4.
- * Rows and columns up to multiples of 16 and 128 are zero, the scales of blocks past the last one 127.
+ * Rows and columns up to multiples of 16 and 128 are zero, the scales of blocks past the last one 127.  A scale of 255, which
+ * cora_quantize_rows never writes, stands for NaN: what its block's numbers are multiplied into is NaN.
  * Limits: rows <= 2^27, cols <= 2^20. */
 typedef struct {
   uint8_t *data, *scale;

@@ -682,7 +682,8 @@ class Rows8:
         groups, blocks = -(-self._rows // 16), -(-self._cols // 128)
         q = self.data.view(torch.float8_e4m3fn).double().view(groups, blocks, 8, 16, 16)
         s = self.scale.view(groups, -1, 16, 4).transpose(2, 3).reshape(groups, -1, 1, 16, 1)[:, :blocks]
-        x = torch.ldexp(q, s.int() - 127).float().permute(0, 3, 1, 2, 4)  # in 64 bits: 2^-127 is no normal float32
+        x = torch.ldexp(q, s.int() - 127).float()  # in 64 bits: 2^-127 is no normal float32
+        x = torch.where(s == 255, torch.nan, x).permute(0, 3, 1, 2, 4)
         return x.reshape(groups * 16, blocks * 128)[:self._rows, :self._cols].contiguous()
 
 

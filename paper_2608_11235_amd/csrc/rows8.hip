@@ -182,7 +182,10 @@ __device__ __forceinline__ f32x4_t mfma_wide(const Wide& w, const Wide& a, f32x4
 #pragma unroll
   for (int t = 0; t < 4; ++t) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.k[t], a.k[t], p, 0, 0, 0);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] += ldexpf(p[e], (int)(ws[e] >> 8 * byte & 255) + (int)(as >> 8 * byte & 255) - 254);
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bw = ws[e] >> 8 * byte & 255, ba = as >> 8 * byte & 255;
+    acc[e] += max(bw, ba) == 255 ? __builtin_nanf("") : ldexpf(p[e], (int)(bw + ba) - 254);
+  }
   return acc;
 }
 
