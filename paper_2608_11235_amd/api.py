@@ -225,6 +225,8 @@ class Model:
         receive the chunk's K and V (cora_forward_cached).  weights: what quantize returned, for products in 8
         bits (cora_forward_quantized), with a workspace of quantized_workspace(chunk.rows) bytes, by default from
         torch's allocator for the call."""
+        if workspace is not None and weights is None:
+            raise ValueError("workspace: only a pass on 8-bit weights takes one")
         device = _device_of(cache, chunk)
         if device != self._device:
             raise ValueError(f"cache: on cuda:{device}, the model is on cuda:{self._device}")
