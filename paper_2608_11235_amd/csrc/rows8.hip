@@ -703,7 +703,7 @@ static double tiles_us(int M, int N, int K, int cfg, int splits, bool wide, int 
 
 // What fits a wavefront's 256 registers: groups of 16 activation rows MB, of weight rows NB, quads of blocks SQ.
 // X(MB, NB, SQ), for results of 8-bit sums and of 32-bit ones
-#define R8_FEW(X) X(1, 1, 1) X(1, 1, 2) X(1, 1, 3) X(1, 2, 1) X(1, 2, 2) X(2, 1, 1) X(2, 1, 2) X(2, 2, 1) X(4, 1, 1)
+#define R8_FEW(X) X(1, 1, 1) X(1, 1, 2) X(1, 1, 3) X(1, 2, 1) X(2, 1, 1) X(2, 1, 2) X(2, 2, 1) X(4, 1, 1)
 #define R8_FEW_WIDE(X) X(1, 1, 1) X(1, 1, 2) X(1, 2, 1) X(2, 1, 1)
 
 static int few_groups(int M, bool wide) { return M <= 16 ? 1 : (M <= 32 || wide ? 2 : 4); }  // MB

@@ -1,6 +1,8 @@
 """The 8-bit products' plans, on the host: the shapes of the GPU tests reach every kernel that a plan can pick, and the layers'
 shapes every way that split sums go on."""
 import ctypes
+import os
+import re
 
 import pytest
 
@@ -61,3 +63,10 @@ def test_layers_hand_on_every_kind_of_sums():
     print(seen)
     assert seen["qkv"] >= {1, 2} and seen["out"] >= {1, 2} and seen["gate_up"] >= {1, 2} and seen["down"] >= {1, 2, 3, 5, 8}
     assert {4, 8} <= seen["qkv"] | seen["out"] | seen["down"]
+
+
+@pytest.mark.parametrize("macro,wide", [("R8_FEW", False), ("R8_FEW_WIDE", True)])
+def test_every_kernel_of_few_rows_is_picked_by_some_size(macro, wide):
+    text = open(os.path.join(os.path.dirname(_lib.__file__), "csrc", "rows8.hip")).read()
+    line = re.search(rf"^#define {macro}\(X\)(.*)$", text, re.M).group(1)
+    assert {tuple(map(int, x)) for x in re.findall(r"X\((\d), (\d), (\d)\)", line)} == FEW[wide]
