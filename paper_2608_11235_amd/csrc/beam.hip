@@ -81,7 +81,8 @@ __device__ __forceinline__ int keep_best(uint64_t* list, int n, int W, uint64_t*
 
 }  // namespace
 
-// 1024 x 152064 in 69 us (4.5 TB/s) with four workgroups of 256 threads a CU: without the candidates 59, without the exponentials 63,
+// 1024 x 152064 in 69 us (4.5 TB/s) with four workgroups of 256 threads a CU; of these (when all sums were fp32) without the
+// candidates 59, without the exponentials 63,
 // without both 57.  Slower were two workgroups of 512 (80), 32 logits a thread (105, in scratch memory), lists of the wavefronts' own
 // in place of the workgroup's barriers (94: four times the candidates) and a cut at 64 or 128 held candidates (72, 79).
 // A row's logits are loaded eight at a time, a tile ahead, whatever its alignment, so that equal rows have equal sums wherever

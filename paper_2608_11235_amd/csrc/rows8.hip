@@ -362,8 +362,9 @@ __global__ __launch_bounds__(512, 2) void k_rows8_few(Rows8ProductArgs g, Rows8F
 //
 // A tile's results pass through LDS of the wavefront's own and leave as runs of CB x 32 bytes, 16 a lane, behind the
 // next tile's first loads (4096 x 37888 bf16 written alone in runs of 32 bytes 81 us, of 64 58 us, of 256 56 us).
-// Bound by the matrix cores and the power that they draw: 8192^3 bf16 in 400 us (2.75 PFLOP/s; on zeros 357),
-// 4096 x 37888 x 3584 in 475 (2.34: the cores busy for 66 % of the cycles), 2048 x 24576 x 4096 in 148 (2.8).
+// Bound by the matrix cores: 8192^3 bf16 in 400 us (2.75 PFLOP/s; on zeros 357, so that the power that they draw costs a tenth),
+// 4096 x 37888 x 3584 in 475 (2.34: the cores busy for 66 % of the cycles; a tenth round on a quarter of the CUs and 310 MB
+// of results account for part of the rest), 2048 x 24576 x 4096 in 148 (2.8).
 // WIDE (sums of 32 bits): a section's fragments are widened to bf16 first, times their scales, the activations all, a group
 // of weight rows at a time; they are free at once, and the barrier stands between.  Bound by the conversions beside the
 // matrix cores: 2048 x 12288 x 4096 in 182 us (1.13 PFLOP/s; 227 with the scales applied to each block's sums).  The results of
@@ -736,9 +737,9 @@ Rows8Plan rows8_plan_tiles(int M, int N, int K, int cfg, int splits, int num_cus
   return p;
 }
 
-// Splits of a product by tiles leave no more than this in the workspace.
-// Two launches have to promise this much: what the estimate gives them is 4 % more than they keep.
+// A second launch's own time, and what two launches have to promise: what the estimate gives them is 4 % more than they keep.
 constexpr double R8_REST_US = 1.5, R8_REST_GAIN = 0.92;
+// Splits of a product by tiles leave no more than this in the workspace.
 constexpr int64_t R8_MOST_PARTS = 1 << 26;
 
 Rows8Plan rows8_plan(int M, int N, int K, bool wide, int num_cus) {
