@@ -123,3 +123,31 @@ def test_equal_logits_leave_the_order_to_the_scores(V):
     token, parent, _ = vocab_beam(x, 2, 7, score.view(-1), width=4)
     ahead = torch.arange(B, device="cuda") * 2 + torch.arange(B, device="cuda") % 2
     assert (parent == ahead[:, None]).all() and (token == torch.arange(4, device="cuda")).all()
+
+
+@pytest.mark.parametrize("B,V", [(4, 4096), (64, 126464), (240, 50257), (600, 50257), (1024, 152064)])
+@pytest.mark.parametrize("kind", ["noise", "8", "16", "30", "60", "one value", "rising", "low first"])
+def test_log_sums(B, V, kind):
+    """A running score of the log sum less the largest logit leaves a best score near zero, which shows the log sum's own
+    error without the score's rounding to fp32."""
+    require_gpu()
+    log_case(f"log sums B={B} V={V} {kind}")
+    x = normal(B + V, B, V)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    each = torch.rand((B, 1), generator=g, device="cuda")
+    if kind == "one value":
+        x = (each * 20 - 10).to(torch.bfloat16).expand(B, V).contiguous()
+    elif kind == "rising":
+        x = (torch.linspace(-9, 9, V, device="cuda") * each).to(torch.bfloat16)
+    elif kind == "low first":
+        x[:, :V // 3] -= 100
+    elif kind != "noise":
+        x[torch.arange(B, device="cuda"), torch.randint(0, V, (B,), generator=g, device="cuda")] = float(kind)
+    below, top = torch.empty(B, dtype=torch.float64, device="cuda"), x.double().amax(1)
+    for r in range(0, B, 128):
+        below[r:r + 128] = torch.log(torch.exp(x[r:r + 128].double() - top[r:r + 128, None]).sum(1))
+    score = below.float()
+    got = vocab_beam(x, 1, -1, score, width=1)[2][:, 0]
+    off = (got.double() - (score.double() - below)).abs()
+    log_case(f"  off by {float(off.max()):.2e} at the most, {float(off.square().mean().sqrt()):.2e} rms")
+    assert float(off.max()) <= 6.7e-7
